@@ -370,6 +370,103 @@ fa_status fa_enqueue_kernel(fa_ctx* ctx, int which, const void* G, int64_t ldg, 
 fa_status fa_aggregate_static(const void* G, int64_t ldg, int p, int64_t n, int dtype, int m,
                               double lambda, int iters, double tol, float* out, void* stream);
 
+/*
+ * The workers' side of the step: what makes the rows of G when the p workers' backward passes run
+ * on one GPU (Alg. 1: worker i computes its minibatch gradient g_i; the aggregator must be given
+ * the p of them, not their sum).  Activations of all workers lie one under the other in matrices
+ * of `rows` rows; worker w owns sizes_host[w] >= 0 consecutive rows, worker 0's first.  Gradients
+ * of parameters are written per worker, worker w's at base + w * ld elements: with base a place in
+ * row 0 of G and ld = ldg they land in the rows that fa_aggregate reads.
+ *
+ * These entry points take no context: the caller passes the stream and, where one is needed, a
+ * device workspace of the size that the matching ..._workspace function returns (16-byte aligned,
+ * free for other use once the call's work on the stream is done).  They allocate nothing, copy
+ * nothing and never synchronise: a call is kernel launches alone and may be captured into a HIP
+ * graph (sizes_host and all scalars are taken at the call).  Calls that share no output and no
+ * workspace may overlap in time.  Runs on the current device.
+ *
+ * Matrices are row-major, unit stride inside a row, `ld` elements from row to row (ld >= width; of
+ * no meaning with one row), at any address that their element type may have.  dtype is the type
+ * of activations and of their gradients, param_dtype of gamma and beta, grad_dtype of the
+ * parameters' gradients (fa_dtype each).  All statistics and sums are fp32, and the results do
+ * not change from run to run.  Outputs must not overlap inputs.  Errors: FA_ERR_ARG (nothing was
+ * enqueued) or FA_ERR_DEVICE.
+ */
+#define FA_CHECKPOINT_BLOCK 32          /* features of a row that share a scale in a checkpoint */
+#define FA_FEATURES_MAX (1 << 18)       /* widest row of a checkpoint or linear layer */
+#define FA_NORM_FEATURES_MAX 16384      /* widest row of a layer norm */
+#define FA_ROWS_MAX ((int64_t)1 << 40)
+
+/*
+ * An activation checkpoint in 8 bits: [rows, features] as codes (int8, rows of
+ * fa_checkpoint_code_pitch(features) bytes: features rounded up to whole blocks of 32) and
+ * exponents (uint8, one for each block, rows of fa_checkpoint_exponent_pitch(features) bytes,
+ * a multiple of four).  Both have no gaps; codes is 16-byte, exponents 4-byte aligned.  With
+ * most = max |v| over a block:
+ *   s = 2^max(floor(log2 most) - 6, -126),  exponent = 127 + log2 s,
+ *   code = v / s rounded to the nearest whole number (ties to even), held within -127..127.
+ * The value is code * s, within s/2 of v (within s where the code was held); it has seven
+ * significant bits and is exact in bf16.  A block with an infinity or a NaN has exponent 255 and
+ * codes 0 and stands for NaN throughout.  Codes past `features` are 0; exponents past the last
+ * block are not written.
+ * fa_checkpoint_pack / fa_checkpoint_unpack convert from and to fp32 or bf16.
+ */
+int64_t fa_checkpoint_code_pitch(int features);
+int64_t fa_checkpoint_exponent_pitch(int features);
+fa_status fa_checkpoint_pack(const void* x, int64_t ldx, int64_t rows, int features, int dtype,
+                             int8_t* codes, uint8_t* exponents, void* stream);
+fa_status fa_checkpoint_unpack(const int8_t* codes, const uint8_t* exponents, int64_t rows,
+                               int features, int dtype, void* x, int64_t ldx, void* stream);
+
+/*
+ * Layer norm of every row: mean = sum x / D, rstd = 1 / sqrt(sum (x - mean)^2 / D + eps),
+ * xhat = (x - mean) rstd, y = xhat gamma + beta.  gamma, beta: `features` parameters or NULL (1
+ * and 0).  mean, rstd: `rows` floats or NULL.  codes, exponents: both NULL, or a checkpoint of
+ * xhat (before gamma and beta) written in the same pass.
+ */
+fa_status fa_layer_norm(const void* x, int64_t ldx, int64_t rows, int features, int dtype,
+                        const void* gamma, const void* beta, int param_dtype, double eps, void* y,
+                        int64_t ldy, float* mean, float* rstd, int8_t* codes, uint8_t* exponents,
+                        void* stream);
+
+/*
+ * Its backward pass.  With h = dy gamma, a = sum h / D, b = sum h xhat / D of a row:
+ *   dx = rstd (h - a - xhat b) [+ residual]   (residual: the gradient that reaches x past the norm)
+ *   dgamma_w = sum of dy xhat, dbeta_w = sum of dy over worker w's rows.
+ * xhat is taken from x with mean and rstd (codes and exponents NULL), or from the checkpoint (x
+ * NULL, mean ignored).  gamma, residual, dgamma, dbeta may be NULL; the workspace is needed with
+ * dgamma or dbeta.  A worker without rows gets zeros.  fa_layer_norm_backward_workspace: bytes,
+ * -1 for bad arguments.
+ */
+int64_t fa_layer_norm_backward_workspace(const int64_t* sizes_host, int p, int features);
+fa_status fa_layer_norm_backward(const void* dy, int64_t lddy, const int64_t* sizes_host, int p,
+                                 int features, int dtype, const void* x, int64_t ldx,
+                                 const float* mean, const float* rstd, const int8_t* codes,
+                                 const uint8_t* exponents, const void* gamma, int param_dtype,
+                                 const void* residual, int64_t ldr, void* dx, int64_t lddx,
+                                 void* dgamma, int64_t lddgamma, void* dbeta, int64_t lddbeta,
+                                 int grad_dtype, void* workspace, int64_t workspace_bytes,
+                                 void* stream);
+
+/*
+ * Weight and bias gradients of a linear layer with `outputs` outputs, from the gradient dy
+ * [rows, outputs] of its outputs and the checkpoint v [rows, features] of its input:
+ *   P_w = sum over worker w's rows of dy^T v (outputs x features), b_w = the same sum of dy,
+ *   dweight_w = P_w,  or with gamma and beta (both or neither; the layer's input was
+ *   v gamma + beta, a checkpointed layer norm's)  dweight_w[o, i] = gamma_i P_w[o, i] + beta_i b_w[o],
+ *   dbias_w = b_w (may be NULL).
+ * Products are exact (bf16 matrix core; fp32 dy in three exact pieces), sums fp32.  A worker
+ * without rows gets zeros.  fa_linear_grad_workspace: bytes (may be 0), -1 for bad arguments.
+ */
+int64_t fa_linear_grad_workspace(const int64_t* sizes_host, int p, int features, int outputs,
+                                 int dtype);
+fa_status fa_linear_grad(const void* dy, int64_t lddy, const int64_t* sizes_host, int p,
+                         int features, int outputs, int dtype, const int8_t* codes,
+                         const uint8_t* exponents, const void* gamma, const void* beta,
+                         int param_dtype, void* dweight, int64_t lddweight, void* dbias,
+                         int64_t lddbias, int grad_dtype, void* workspace, int64_t workspace_bytes,
+                         void* stream);
+
 const char* fa_status_string(fa_status s);
 const char* fa_version(void);
 

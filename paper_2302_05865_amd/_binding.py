@@ -27,6 +27,9 @@ EXPORTED_SYMBOLS = (
     "fa_get_timings", "fa_enqueue_kernel", "fa_aggregate_restream", "fa_get_restream_info",
     "fa_status_string", "fa_version", "fa_aggregate_static", "fa_gram_begin", "fa_gram_update", "fa_gram_update_rows",
     "fa_aggregate_arrived",
+    "fa_checkpoint_code_pitch", "fa_checkpoint_exponent_pitch", "fa_checkpoint_pack",
+    "fa_checkpoint_unpack", "fa_layer_norm", "fa_layer_norm_backward_workspace",
+    "fa_layer_norm_backward", "fa_linear_grad_workspace", "fa_linear_grad",
 )
 
 
@@ -101,6 +104,26 @@ def load_library() -> ctypes.CDLL:
     lib.fa_gram_update_rows.restype = i32
     lib.fa_aggregate_arrived.argtypes = [vp, vp, i64, i32, dbl, i32, dbl, vp]
     lib.fa_aggregate_arrived.restype = i32
+    lib.fa_checkpoint_code_pitch.argtypes = [i32]
+    lib.fa_checkpoint_code_pitch.restype = i64
+    lib.fa_checkpoint_exponent_pitch.argtypes = [i32]
+    lib.fa_checkpoint_exponent_pitch.restype = i64
+    lib.fa_checkpoint_pack.argtypes = [vp, i64, i64, i32, i32, vp, vp, vp]
+    lib.fa_checkpoint_pack.restype = i32
+    lib.fa_checkpoint_unpack.argtypes = [vp, vp, i64, i32, i32, vp, i64, vp]
+    lib.fa_checkpoint_unpack.restype = i32
+    lib.fa_layer_norm.argtypes = [vp, i64, i64, i32, i32, vp, vp, i32, dbl, vp, i64, vp, vp, vp, vp, vp]
+    lib.fa_layer_norm.restype = i32
+    lib.fa_layer_norm_backward_workspace.argtypes = [vp, i32, i32]
+    lib.fa_layer_norm_backward_workspace.restype = i64
+    lib.fa_layer_norm_backward.argtypes = [vp, i64, vp, i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, i32, vp, i64,
+                                           vp, i64, vp, i64, vp, i64, i32, vp, i64, vp]
+    lib.fa_layer_norm_backward.restype = i32
+    lib.fa_linear_grad_workspace.argtypes = [vp, i32, i32, i32, i32]
+    lib.fa_linear_grad_workspace.restype = i64
+    lib.fa_linear_grad.argtypes = [vp, i64, vp, i32, i32, i32, i32, vp, vp, vp, vp, i32, vp, i64, vp, i64, i32,
+                                   vp, i64, vp]
+    lib.fa_linear_grad.restype = i32
     lib.fa_status_string.argtypes = [i32]
     lib.fa_status_string.restype = ctypes.c_char_p
     lib.fa_version.argtypes = []

@@ -11,6 +11,8 @@ FA_WORKER_MAJOR, FA_ROW_MAJOR = 0, 1
 FA_SOLVER_AUTO, FA_SOLVER_JACOBI16, FA_SOLVER_JACOBI = 0, 1, 2
 FA_GRAM_AUTO, FA_GRAM_FP64, FA_GRAM_BF16_MATRIX = 0, 1, 2
 FA_GRAM_AUTO_MIN_ROWS = 1 << 20
+FA_CHECKPOINT_BLOCK = 32
+FA_FEATURES_MAX, FA_NORM_FEATURES_MAX = 1 << 18, 16384
 
 
 class FaConfig(ctypes.Structure):

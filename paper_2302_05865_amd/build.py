@@ -24,6 +24,9 @@ SOURCES = {
     "fa_irls64.hip": [],
     "fa_gram_lp.hip": [],
     "fa_api.hip": [],
+    "fa_layer_norm.hip": [],
+    "fa_linear_grad.hip": [],
+    "fa_layers_api.hip": [],
 }
 OBJ_DIR = os.path.join(HERE, "_build")
 

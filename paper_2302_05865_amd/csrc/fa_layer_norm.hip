@@ -1,0 +1,426 @@
+// Layer norm over the rows of p workers, its backward pass, and the 8-bit checkpoint between the two.
+//
+//   mu = sum_j x_j / D,  var = sum_j (x_j - mu)^2 / D,  r = 1 / sqrt(var + eps),  xhat = (x - mu) r,  y = xhat gamma + beta
+//   h = dy gamma,  a = sum_j h_j / D,  b = sum_j h_j xhat_j / D,  dx = r (h - a - xhat b) [+ residual]
+//   dgamma_w = sum over the rows of worker w of dy xhat,  dbeta_w = the same of dy
+//
+// A row is held in registers by a team of lanes, eight consecutive features a lane and piece: every row is read once,
+// the variance is that of the centred values, and four neighbouring lanes hold one block of a checkpoint.  Statistics and
+// sums are fp32.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "fa.h"
+#include "fa_layers.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// sum over a team of L lanes (a power of two of one wavefront)
+template <int L>
+__device__ __forceinline__ float team_sum(float v) {
+#pragma unroll
+  for (int d = 1; d < L; d *= 2) v += __shfl_xor(v, d);
+  return v;
+}
+
+}  // namespace
+
+// T: storage of x and y; a row's team is L lanes of a wavefront (W = 1) or W whole wavefronts, with NC pieces of eight
+// features a lane.
+template <typename T, int L, int NC, int W>
+__global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_kernel(fa_norm_args a) {
+  static_assert(W == 1 || L == 64, "a team of several wavefronts uses all their lanes");
+  constexpr int TL = L * W;                                    // lanes of a team
+  constexpr int TEAMS = W > 1 ? 1 : kThreads / L;
+  __shared__ float red[2][W];
+  const int lane = threadIdx.x % TL, D = a.features;
+  const float width = (float)D;
+  for (int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TL; row < a.rows; row += (int64_t)gridDim.x * TEAMS) {
+    const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+    float v[NC][8];
+    float s = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int at = 8 * (lane + TL * c);
+      fa_load8(x + at, D - at, v[c]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += v[c][e];
+    }
+    s = team_sum<L>(s);
+    if constexpr (W > 1) {
+      if (threadIdx.x % 64 == 0) red[0][threadIdx.x / 64] = s;
+      __syncthreads();
+      s = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) s += red[0][w];
+    }
+    const float mean = s / width;
+    float q = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int at = 8 * (lane + TL * c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[c][e] = at + e < D ? v[c][e] - mean : 0.f;
+        q += v[c][e] * v[c][e];
+      }
+    }
+    q = team_sum<L>(q);
+    if constexpr (W > 1) {
+      if (threadIdx.x % 64 == 0) red[1][threadIdx.x / 64] = q;
+      __syncthreads();
+      q = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) q += red[1][w];
+    }
+    const float rstd = 1.f / sqrtf(q / width + a.eps);
+    if (lane == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
+    T* y = static_cast<T*>(a.y) + row * a.ldy;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int at = 8 * (lane + TL * c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[c][e] = at + e < D ? v[c][e] * rstd : 0.f;
+      if (a.codes) {
+        const uint32_t e = fa_block_exponent(fa_quad_most(v[c]));
+        const int64_t pitch = fa_code_pitch(D);
+        if (at < pitch) {
+          *reinterpret_cast<uint2*>(a.codes + row * pitch + at) = fa_codes8(v[c], e);
+          if ((lane & 3) == 0) a.exponents[row * fa_exponent_pitch(D) + (at >> 5)] = (uint8_t)e;
+        }
+      }
+      float g[8], b[8];
+      if (a.gamma) {
+        fa_load8_param(a.gamma, a.param_bf16, at, D - at, g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[c][e] *= g[e];
+      }
+      if (a.beta) {
+        fa_load8_param(a.beta, a.param_bf16, at, D - at, b);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[c][e] += b[e];
+      }
+      fa_store8(y + at, D - at, v[c]);
+    }
+  }
+}
+
+namespace {
+
+// Rows that one workgroup of the backward pass takes: a share of one worker's.  About kNormBlocks workgroups in all.
+constexpr int kNormBlocks = 1024;
+
+struct norm_chunks {
+  int first[FA_P_MAX + 1];   // worker w has the chunks [first[w], first[w + 1])
+  int64_t rows_per_chunk;
+};
+
+norm_chunks cut(const fa_row_blocks& b, int64_t rows) {
+  norm_chunks c;
+  c.rows_per_chunk = (rows + kNormBlocks - 1) / kNormBlocks;
+  if (c.rows_per_chunk < 4) c.rows_per_chunk = 4;
+  c.first[0] = 0;
+  for (int w = 0; w < FA_P_MAX; ++w)
+    c.first[w + 1] = c.first[w] + (w < b.p ? (int)((b.row0[w + 1] - b.row0[w] + c.rows_per_chunk - 1) / c.rows_per_chunk) : 0);
+  return c;
+}
+
+// the worker that chunk k belongs to: as many workers end at or before it as come ahead of it
+__device__ __forceinline__ int worker_of(const int* first, int p, int k) {
+  int w = 0;
+  for (int j = 1; j < p; ++j) w += first[j] <= k ? 1 : 0;
+  return w;
+}
+
+}  // namespace
+
+// T: storage of dy, x, dx; KEPT: xhat from the checkpoint.  One workgroup takes one chunk of rows of one worker and leaves
+// its share of dgamma and dbeta in partials[chunk][2][D].
+template <typename T, bool KEPT, int L, int NC, int W>
+__global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_backward_kernel(fa_norm_grad_args a, norm_chunks ch) {
+  constexpr int TL = L * W;
+  constexpr int THREADS = W > 1 ? 64 * W : kThreads;
+  constexpr int TEAMS = THREADS / TL;
+  constexpr int WAVES = THREADS / 64;
+  __shared__ float2 red[2][WAVES];
+  __shared__ float join[W > 1 ? 1 : WAVES * 2 * L * NC * 8];
+  const int lane = threadIdx.x % TL, D = a.features;
+  const float width = (float)D;
+  const int64_t pitch = fa_code_pitch(D), epitch = fa_exponent_pitch(D);
+  const int w = worker_of(ch.first, a.blocks.p, blockIdx.x);
+  const int64_t begin = a.blocks.row0[w] + (int64_t)(blockIdx.x - ch.first[w]) * ch.rows_per_chunk;
+  const int64_t end = min(begin + ch.rows_per_chunk, a.blocks.row0[w + 1]);
+  float dg[NC][8], db[NC][8];
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dg[c][e] = db[c][e] = 0.f;
+  int turn = 0;
+  for (int64_t row = begin + threadIdx.x / TL; row < end; row += TEAMS, turn ^= 1) {
+    const T* dy = static_cast<const T*>(a.dy) + row * a.lddy;
+    const float rstd = a.rstd[row];
+    float xh[NC][8], h[NC][8];
+    float s = 0.f, q = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int at = 8 * (lane + TL * c);
+      fa_load8(dy + at, D - at, h[c]);
+      if constexpr (KEPT) {
+        if (at < pitch) {
+          const uint2 codes = *reinterpret_cast<const uint2*>(a.codes + row * pitch + at);
+          fa_values8(codes, fa_block_scale(a.exponents[row * epitch + (at >> 5)]), xh[c]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) xh[c][e] = 0.f;
+        }
+      } else {
+        fa_load8(static_cast<const T*>(a.x) + row * a.ldx + at, D - at, xh[c]);
+        const float mean = a.mean[row];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) xh[c][e] = (xh[c][e] - mean) * rstd;
+      }
+      float g[8];
+      if (a.gamma) fa_load8_param(a.gamma, a.param_bf16, at, D - at, g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (at + e < D) {
+          db[c][e] += h[c][e];
+          dg[c][e] += h[c][e] * xh[c][e];
+          if (a.gamma) h[c][e] *= g[e];
+          s += h[c][e];
+          q += h[c][e] * xh[c][e];
+        }
+      }
+    }
+    s = team_sum<L>(s);
+    q = team_sum<L>(q);
+    if constexpr (W > 1) {
+      // (two slots in turn: a wavefront is past the next row's barrier before anyone writes this slot again)
+      if (threadIdx.x % 64 == 0) red[turn][threadIdx.x / 64] = make_float2(s, q);
+      __syncthreads();
+      s = q = 0.f;
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        s += red[turn][k].x;
+        q += red[turn][k].y;
+      }
+    }
+    s /= width;
+    q /= width;
+    T* dx = static_cast<T*>(a.dx) + row * a.lddx;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int at = 8 * (lane + TL * c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[c][e] = rstd * (h[c][e] - s - xh[c][e] * q);
+      if (a.residual) {
+        float r[8];
+        fa_load8(static_cast<const T*>(a.residual) + row * a.ldr + at, D - at, r);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[c][e] += r[e];
+      }
+      fa_store8(dx + at, D - at, h[c]);
+    }
+  }
+  if (!a.dgamma && !a.dbeta) return;
+  float* part = a.partials + (int64_t)blockIdx.x * 2 * D;
+  if constexpr (W > 1) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int at = 8 * (lane + TL * c);
+      fa_store8(part + at, D - at, dg[c]);
+      fa_store8(part + D + at, D - at, db[c]);
+    }
+  } else {
+    // the teams of a wavefront by shuffles, then the wavefronts through LDS, in their order
+    constexpr int SPAN = L * NC * 8;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int d = L; d < 64; d *= 2) {
+          dg[c][e] += __shfl_xor(dg[c][e], d);
+          db[c][e] += __shfl_xor(db[c][e], d);
+        }
+    if (threadIdx.x % 64 < L) {
+      float* mine = join + (threadIdx.x / 64) * 2 * SPAN;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          mine[8 * (lane + L * c) + e] = dg[c][e];
+          mine[SPAN + 8 * (lane + L * c) + e] = db[c][e];
+        }
+    }
+    __syncthreads();
+    for (int k = threadIdx.x; k < 2 * D; k += THREADS) {
+      const int at = k < D ? k : SPAN + k - D;
+      float s = 0.f;
+#pragma unroll
+      for (int v = 0; v < WAVES; ++v) s += join[v * 2 * SPAN + at];
+      part[k] = s;
+    }
+  }
+}
+
+// dgamma (blockIdx.z = 0) and dbeta (1) of one worker: its chunks' shares, four interleaved sums joined in their order.
+__global__ __launch_bounds__(kThreads) void fa_layer_norm_grads_kernel(fa_norm_grad_args a, norm_chunks ch) {
+  __shared__ float red[4][64];
+  const int w = blockIdx.y, which = blockIdx.z, D = a.features;
+  void* out = which ? a.dbeta : a.dgamma;
+  if (!out) return;
+  const int j = blockIdx.x * 64 + threadIdx.x % 64, group = threadIdx.x / 64;
+  float s = 0.f;
+  if (j < D)
+    for (int k = ch.first[w] + group; k < ch.first[w + 1]; k += 4) s += a.partials[((int64_t)k * 2 + which) * D + j];
+  red[group][threadIdx.x % 64] = s;
+  __syncthreads();
+  if (group == 0 && j < D) {
+    s = red[0][threadIdx.x] + red[1][threadIdx.x] + red[2][threadIdx.x] + red[3][threadIdx.x];
+    const int64_t at = (int64_t)w * (which ? a.lddbeta : a.lddgamma) + j;
+    if (a.grad_bf16) fa_store1(static_cast<fa_bf16*>(out) + at, s);
+    else fa_store1(static_cast<float*>(out) + at, s);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void fa_checkpoint_pack_kernel(const T* x, int64_t ldx, int64_t rows, int D, int8_t* codes,
+                                                                      uint8_t* exponents) {
+  // a thread for every eight codes of a padded row: four of them are one block, whichever row they are in
+  const int64_t pitch = fa_code_pitch(D), epitch = fa_exponent_pitch(D);
+  const int64_t per_row = pitch / 8, total = rows * per_row;
+  const int64_t whole = (total + 63) / 64 * 64;   // (all lanes of a wavefront stay for the exchange between lanes)
+  for (int64_t k = (int64_t)blockIdx.x * kThreads + threadIdx.x; k < whole; k += (int64_t)gridDim.x * kThreads) {
+    const int64_t row = k / per_row;
+    const int at = 8 * (int)(k - row * per_row);
+    float v[8];
+    fa_load8(x + row * ldx + at, k < total ? D - at : 0, v);
+    const uint32_t e = fa_block_exponent(fa_quad_most(v));
+    if (k < total) {
+      *reinterpret_cast<uint2*>(codes + row * pitch + at) = fa_codes8(v, e);
+      if ((k & 3) == 0) exponents[row * epitch + (at >> 5)] = (uint8_t)e;
+    }
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void fa_checkpoint_unpack_kernel(const int8_t* codes, const uint8_t* exponents, int64_t rows,
+                                                                        int D, T* x, int64_t ldx) {
+  const int64_t pitch = fa_code_pitch(D), epitch = fa_exponent_pitch(D);
+  const int64_t per_row = pitch / 8, total = rows * per_row;
+  for (int64_t k = (int64_t)blockIdx.x * kThreads + threadIdx.x; k < total; k += (int64_t)gridDim.x * kThreads) {
+    const int64_t row = k / per_row;
+    const int at = 8 * (int)(k - row * per_row);
+    float v[8];
+    fa_values8(*reinterpret_cast<const uint2*>(codes + row * pitch + at), fa_block_scale(exponents[row * epitch + (at >> 5)]), v);
+    fa_store8(x + row * ldx + at, D - at, v);
+  }
+}
+
+namespace {
+
+int grid_for(int64_t threads) {
+  const int64_t blocks = (threads + kThreads - 1) / kThreads;
+  return (int)(blocks < 1 ? 1 : blocks > 8192 ? 8192 : blocks);
+}
+
+template <typename T, int L, int NC, int W>
+hipError_t norm(const fa_norm_args& a, hipStream_t st) {
+  const int teams = W > 1 ? 1 : kThreads / L;
+  int64_t blocks = (a.rows + teams - 1) / teams;
+  if (blocks > 4096) blocks = 4096;
+  hipLaunchKernelGGL((fa_layer_norm_kernel<T, L, NC, W>), dim3((unsigned)blocks), dim3(W > 1 ? 64 * W : kThreads), 0, st, a);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t norm_of(const fa_norm_args& a, hipStream_t st) {
+  const int D = a.features;
+  if (D <= 32) return norm<T, 4, 1, 1>(a, st);
+  if (D <= 128) return norm<T, 16, 1, 1>(a, st);
+  if (D <= 512) return norm<T, 64, 1, 1>(a, st);
+  if (D <= 1024) return norm<T, 64, 2, 1>(a, st);
+  if (D <= 2048) return norm<T, 64, 4, 1>(a, st);
+  if (D <= 4096) return norm<T, 64, 2, 4>(a, st);
+  if (D <= 8192) return norm<T, 64, 4, 4>(a, st);
+  return norm<T, 64, 8, 4>(a, st);
+}
+
+template <typename T, bool KEPT, int L, int NC, int W>
+void norm_backward(const fa_norm_grad_args& a, const norm_chunks& ch, hipStream_t st) {
+  hipLaunchKernelGGL((fa_layer_norm_backward_kernel<T, KEPT, L, NC, W>), dim3((unsigned)ch.first[FA_P_MAX]),
+                     dim3(W > 1 ? 64 * W : kThreads), 0, st, a, ch);
+}
+
+template <typename T, bool KEPT>
+void norm_backward_of(const fa_norm_grad_args& a, const norm_chunks& ch, hipStream_t st) {
+  const int D = a.features;
+  if (D <= 32) norm_backward<T, KEPT, 4, 1, 1>(a, ch, st);
+  else if (D <= 128) norm_backward<T, KEPT, 16, 1, 1>(a, ch, st);
+  else if (D <= 512) norm_backward<T, KEPT, 64, 1, 1>(a, ch, st);
+  else if (D <= 1024) norm_backward<T, KEPT, 64, 2, 1>(a, ch, st);
+  else if (D <= 2048) norm_backward<T, KEPT, 64, 1, 4>(a, ch, st);
+  else if (D <= 4096) norm_backward<T, KEPT, 64, 2, 4>(a, ch, st);
+  else if (D <= 8192) norm_backward<T, KEPT, 64, 4, 4>(a, ch, st);
+  else norm_backward<T, KEPT, 64, 4, 8>(a, ch, st);
+}
+
+}  // namespace
+
+hipError_t fa_launch_checkpoint_pack(const void* x, int64_t ldx, int64_t rows, int features, int dtype, int8_t* codes,
+                                     uint8_t* exponents, hipStream_t st) {
+  const dim3 grid(grid_for(rows * (fa_code_pitch(features) / 8))), block(kThreads);
+  if (dtype == FA_F32)
+    hipLaunchKernelGGL(fa_checkpoint_pack_kernel<float>, grid, block, 0, st, static_cast<const float*>(x), ldx, rows, features,
+                       codes, exponents);
+  else
+    hipLaunchKernelGGL(fa_checkpoint_pack_kernel<fa_bf16>, grid, block, 0, st, static_cast<const fa_bf16*>(x), ldx, rows, features,
+                       codes, exponents);
+  return hipGetLastError();
+}
+
+hipError_t fa_launch_checkpoint_unpack(const int8_t* codes, const uint8_t* exponents, int64_t rows, int features, int dtype,
+                                       void* x, int64_t ldx, hipStream_t st) {
+  const dim3 grid(grid_for(rows * (fa_code_pitch(features) / 8))), block(kThreads);
+  if (dtype == FA_F32)
+    hipLaunchKernelGGL(fa_checkpoint_unpack_kernel<float>, grid, block, 0, st, codes, exponents, rows, features,
+                       static_cast<float*>(x), ldx);
+  else
+    hipLaunchKernelGGL(fa_checkpoint_unpack_kernel<fa_bf16>, grid, block, 0, st, codes, exponents, rows, features,
+                       static_cast<fa_bf16*>(x), ldx);
+  return hipGetLastError();
+}
+
+hipError_t fa_launch_layer_norm(const fa_norm_args& a, int dtype, hipStream_t st) {
+  return dtype == FA_F32 ? norm_of<float>(a, st) : norm_of<fa_bf16>(a, st);
+}
+
+size_t fa_layer_norm_partials(const fa_row_blocks& b, int64_t rows, int features) {
+  return sizeof(float) * 2 * (size_t)cut(b, rows).first[FA_P_MAX] * (size_t)features;
+}
+
+hipError_t fa_launch_layer_norm_backward(const fa_norm_grad_args& a, int dtype, hipStream_t st) {
+  const norm_chunks ch = cut(a.blocks, a.rows);
+  if (a.rows > 0) {
+    const bool kept = a.x == nullptr;
+    if (dtype == FA_F32) {
+      if (kept) norm_backward_of<float, true>(a, ch, st);
+      else norm_backward_of<float, false>(a, ch, st);
+    } else {
+      if (kept) norm_backward_of<fa_bf16, true>(a, ch, st);
+      else norm_backward_of<fa_bf16, false>(a, ch, st);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (a.dgamma || a.dbeta)
+    hipLaunchKernelGGL(fa_layer_norm_grads_kernel, dim3((unsigned)((a.features + 63) / 64), (unsigned)a.blocks.p, 2),
+                       dim3(kThreads), 0, st, a, ch);
+  return hipGetLastError();
+}
