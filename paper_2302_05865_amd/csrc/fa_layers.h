@@ -62,14 +62,14 @@ hipError_t fa_launch_checkpoint_unpack(const int8_t* codes, const uint8_t* expon
 hipError_t fa_launch_layer_norm(const fa_norm_args& a, int dtype, hipStream_t st);
 size_t fa_layer_norm_partials(const fa_row_blocks& b, int64_t rows, int features);
 hipError_t fa_launch_layer_norm_backward(const fa_norm_grad_args& a, int dtype, hipStream_t st);
-int fa_linear_grad_splits(const fa_row_blocks& b, int features, int outputs, int dtype);
-size_t fa_linear_grad_partials(const fa_row_blocks& b, int features, int outputs, int splits);
-hipError_t fa_launch_linear_grad(const fa_linear_grad_args& a, int dtype, hipStream_t st);
+size_t fa_linear_grad_partials(const fa_row_blocks& b, int features, int outputs, int dtype);
+hipError_t fa_launch_linear_grad(fa_linear_grad_args a, int dtype, hipStream_t st);   // (a.splits is the launcher's)
 
 #ifdef __HIPCC__
 // ---- eight consecutive elements, at any alignment that the element type has (global memory takes 16-byte accesses
 // at any address), as float -------------------------------------------------------------------------------------------
 typedef uint32_t fa_u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t fa_u32x2 __attribute__((ext_vector_type(2)));
 typedef fa_u32x4 fa_u32x4_2 __attribute__((aligned(2)));
 typedef fa_u32x4 fa_u32x4_4 __attribute__((aligned(4)));
 typedef float fa_f32x2 __attribute__((ext_vector_type(2)));

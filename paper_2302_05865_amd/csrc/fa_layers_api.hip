@@ -125,7 +125,7 @@ extern "C" int64_t fa_linear_grad_workspace(const int64_t* sizes_host, int p, in
   if (!known(dtype) || !row_blocks(sizes_host, p, &b) || !extent(0, features, FA_FEATURES_MAX) ||
       !extent(0, outputs, FA_FEATURES_MAX))
     return -1;
-  return (int64_t)fa_linear_grad_partials(b, features, outputs, fa_linear_grad_splits(b, features, outputs, dtype));
+  return (int64_t)fa_linear_grad_partials(b, features, outputs, dtype);
 }
 
 extern "C" fa_status fa_linear_grad(const void* dy, int64_t lddy, const int64_t* sizes_host, int p, int features, int outputs,
@@ -142,12 +142,11 @@ extern "C" fa_status fa_linear_grad(const void* dy, int64_t lddy, const int64_t*
       !matrix(dweight, lddweight, p, (int64_t)outputs * features, grad_dtype) ||
       (dbias && !matrix(dbias, lddbias, p, outputs, grad_dtype)))
     return FA_ERR_ARG;
-  a.splits = fa_linear_grad_splits(a.blocks, features, outputs, dtype);
-  const int64_t need = (int64_t)fa_linear_grad_partials(a.blocks, features, outputs, a.splits);
+  const int64_t need = (int64_t)fa_linear_grad_partials(a.blocks, features, outputs, dtype);
   if (need > 0 && (!workspace || ((uintptr_t)workspace & 15u) != 0 || workspace_bytes < need)) return FA_ERR_ARG;
   a.dy = dy; a.gamma = gamma; a.beta = beta; a.codes = codes; a.exponents = exponents;
   a.dweight = dweight; a.dbias = dbias; a.partials = static_cast<float*>(workspace);
   a.lddy = lddy; a.lddweight = lddweight; a.lddbias = lddbias;
-  a.features = features; a.outputs = outputs; a.param_bf16 = param_dtype == FA_BF16; a.grad_bf16 = grad_dtype == FA_BF16;
+  a.features = features; a.outputs = outputs; a.splits = 1; a.param_bf16 = param_dtype == FA_BF16; a.grad_bf16 = grad_dtype == FA_BF16;
   return fa_launch_linear_grad(a, dtype, (hipStream_t)stream) == hipSuccess ? FA_OK : FA_ERR_DEVICE;
 }

@@ -5,8 +5,8 @@
 //
 // where v are the checkpoint's values.  They have seven significant bits, so they are exact in bf16; dY is bf16, or fp32
 // cut exactly into three pieces of eight bits.  Every product on the bf16 matrix core is exact, sums are fp32.  The rows are
-// the contracted index of both operands and lie far apart in memory: the tiles go to LDS as they lie and are read through
-// the transposing LDS load.
+// the contracted index of both operands and lie far apart in memory; a lane of the matrix instruction takes eight
+// consecutive ones of a column, so tiles are turned on their way to LDS.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -18,10 +18,7 @@ namespace {
 constexpr int kThreads = 256;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 // x = h + m + l exactly, each with eight significant bits, h and m cut off (h of the largest finite value stays finite).
 // An infinity or a NaN is h, with nothing left over.
@@ -42,39 +39,122 @@ __device__ __forceinline__ uint32_t upper_halves(uint32_t a, uint32_t b) { retur
 
 // A workgroup makes a tile of BM outputs x BN features of one worker (of one split of its rows); its four wavefronts a
 // quarter each, 32 x 32 results at a time.  T: storage of dY.
+//
+// Rows come in steps of BK.  While the matrix core works on one step in LDS, the next one, already in registers, is made
+// into the other half of LDS and the one after it is on its way from memory: one barrier a step, no wait on memory.  A
+// thread brings in 8 rows of a few outputs of dY and 8 rows of a few codes, and turns them on the way: LDS holds, for
+// every output (feature), the BK values of the contracted index in pieces of 8, which is what a lane of the matrix
+// instruction takes with one 16-byte read.  Piece c of column j lies at place c ^ swizzle(j): 16 lanes that read one
+// piece of 16 neighbouring columns, and 8 that write one piece of every eighth column, meet no bank twice.
+namespace {
+
 template <typename T, int BM, int BN, int BK>
-__global__ __launch_bounds__(kThreads) void fa_linear_grad_kernel(fa_linear_grad_args a) {
-  constexpr int PLANES = sizeof(T) == 4 ? 3 : 1;
-  constexpr int AP = BM * 2 + 32, BP = BN * 2 + 32;       // LDS bytes of a row (+32: rows of one read on their own banks)
+struct tile {
+  static constexpr int PLANES = sizeof(T) == 4 ? 3 : 1;
+  static constexpr int ROW = BK * 2;                           // LDS bytes of a column
+  static constexpr int A_BYTES = BM * ROW * PLANES, B_BYTES = BN * ROW;   // of one step; LDS: dY, dY, codes, codes
+  static constexpr int PIECES = BK / 8;
+  // a thread's unit of dY is 8 rows of AC outputs, its unit of codes 8 rows of BC features
+  static constexpr int AC = BM * PIECES / kThreads, BC = BN * PIECES / kThreads;
+  static constexpr int AW = AC * (int)sizeof(T) / 4, BW = BC / 4;           // dwords of a row of it
+  static_assert((AW == 2 || AW == 4) && (BW == 1 || BW == 2), "loads of 8 or 16, and of 4 or 8 bytes");
+  static_assert(PIECES == 8, "swizzle() is for eight pieces");
+};
+
+__device__ __forceinline__ int swizzle(int column) { return ((column >> 1) ^ (column >> 3)) & 7; }
+
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");   // (loads from memory stay in flight)
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+template <int N>
+using words = uint32_t __attribute__((ext_vector_type(N)));
+
+template <int N>
+__device__ __forceinline__ words<N> load_words(const unsigned char* p) {   // at any address
+  words<N> u;
+  __builtin_memcpy(&u, p, sizeof(u));
+  return u;
+}
+// a unit's row of dY of which the first `valid` elements exist, zeros behind them
+template <int N>
+__device__ __forceinline__ words<N> load_some(const fa_bf16* p, int valid) {
+  words<N> u = {};
+  if (valid >= 2 * N) return load_words<N>(reinterpret_cast<const unsigned char*>(p));
+#pragma unroll
+  for (int e = 0; e < 2 * N; ++e)
+    if (e < valid) u[e >> 1] |= (uint32_t)p[e].bits << (16 * (e & 1));
+  return u;
+}
+template <int N>
+__device__ __forceinline__ words<N> load_some(const float* p, int valid) {
+  words<N> u = {};
+  if (valid >= N) return load_words<N>(reinterpret_cast<const unsigned char*>(p));
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (e < valid) u[e] = __float_as_uint(p[e]);
+  return u;
+}
+
+// s + the sum of eight bf16 values, in fp32
+__device__ __forceinline__ float add8(bf16x8 v, float s) {
+  const fa_bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
+  const fa_u32x4 u = __builtin_bit_cast(fa_u32x4, v);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(fa_bf16x2, (uint32_t)u[e]), one, s, false);
+  return s;
+}
+
+}  // namespace
+
+template <typename T, int BM, int BN, int BK>
+__global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_grad_args a) {
+  using S = tile<T, BM, BN, BK>;
   constexpr int FM = BM / 64, FN = BN / 64;               // 32 x 32 results of a wavefront in either direction
-  __shared__ __attribute__((aligned(16))) unsigned char la[PLANES][BK * AP];
-  __shared__ __attribute__((aligned(16))) unsigned char lb[BK * BP];
-  __shared__ float bias[BM];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int HM = FM > 1 ? FM / 2 : 1;                 // of the FM, those whose column sums a wavefront makes
+  constexpr int AC = S::AC, KK = BK / 16;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2 * (S::A_BYTES + S::B_BYTES)];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int tiles_o = (a.outputs + BM - 1) / BM, tiles_i = (a.features + BN - 1) / BN;
-  int64_t k = blockIdx.x;
-  const int ti = (int)(k % tiles_i);
-  k /= tiles_i;
-  const int to = (int)(k % tiles_o);
-  k /= tiles_o;
-  const int split = (int)(k % a.splits), w = (int)(k / a.splits);
+  int64_t id = blockIdx.x;
+  const int ti = (int)(id % tiles_i);
+  id /= tiles_i;
+  const int to = (int)(id % tiles_o);
+  id /= tiles_o;
+  const int split = (int)(id % a.splits), w = (int)(id / a.splits);
   const int o0 = to * BM, i0 = ti * BN;
   // this split's rows: whole steps of BK rows
   const int64_t all = a.blocks.row0[w + 1] - a.blocks.row0[w];
-  const int64_t steps = (all + BK - 1) / BK, per = (steps + a.splits - 1) / a.splits;
+  const int64_t steps_all = (all + BK - 1) / BK, per = (steps_all + a.splits - 1) / a.splits;
   const int64_t begin = a.blocks.row0[w] + min(all, (int64_t)split * per * BK);
   const int64_t end = a.blocks.row0[w] + min(all, ((int64_t)split + 1) * per * BK);
   const int64_t pitch = fa_code_pitch(a.features), epitch = fa_exponent_pitch(a.features);
 
-  // what a thread brings in: pieces of 8 outputs of dY, pieces of 16 codes
-  constexpr int A_PER_ROW = BM / 8, A_ROWS = kThreads / A_PER_ROW, A_N = BK / A_ROWS;
-  constexpr int B_PER_ROW = BN / 16, B_ROWS = kThreads / B_PER_ROW, B_N = BK / B_ROWS;
-  static_assert(A_N * A_ROWS == BK && B_N * B_ROWS == BK, "whole rounds of loads");
-  const int ac = (tid % A_PER_ROW) * 8, ar = tid / A_PER_ROW;
-  const int bc = (tid % B_PER_ROW) * 16, br = tid / B_PER_ROW;
-  float sum[8];
+  // The unit of dY and the unit of codes that this thread brings in: rows 8 piece.., columns.  Columns past the matrix
+  // take part like any other and are not written at the end, so all that matters is that what is read for them is
+  // there: a unit beyond the last column reads the tile's first one, one that the last column is in reads on into the
+  // next row.  The last rows of the whole matrix have no such next row: those, and steps that are not whole, are taken
+  // element by element behind the others.
+  const int a_col = tid % (BM / AC) * AC, a_piece = tid / (BM / AC);
+  const int b_col = tid % (BN / S::BC) * S::BC, b_piece = tid / (BN / S::BC);
+  const int64_t over = (AC - a.outputs % AC) % AC;        // elements of the last unit past the last column
+  const int64_t reach = a.blocks.row0[a.blocks.p] - (over + a.lddy - 1) / a.lddy;
+  const int64_t fast = a.lddy < (1 << 24) && min(end, reach) > begin ? (min(end, reach) - begin) / BK : 0;
+  const int64_t steps = (end - begin + BK - 1) / BK;
+  const uint32_t a_off = (uint32_t)((int64_t)a_piece * 8 * a.lddy + (o0 + a_col < a.outputs ? a_col : 0)) * (uint32_t)sizeof(T);
+  const int b_safe = i0 + b_col < pitch ? b_col : 0;
+  const uint32_t b_off = (uint32_t)(b_piece * 8 * (int)pitch + b_safe);
+  const uint32_t e_off = (uint32_t)(b_piece * 8 * (int)epitch + (b_safe >> 5));
+  using AR = words<S::AW>;
+  using BR = words<S::BW>;
+  AR raw_a[2][8];
+  BR raw_b[2][8];
+  uint32_t raw_e[2][8];
+  float sum[HM];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+  for (int m = 0; m < HM; ++m) sum[m] = 0.f;
   f32x16 acc[FM][FN];
 #pragma unroll
   for (int m = 0; m < FM; ++m)
@@ -82,94 +162,177 @@ __global__ __launch_bounds__(kThreads) void fa_linear_grad_kernel(fa_linear_grad
     for (int n = 0; n < FN; ++n)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[m][n][r] = 0.f;
-  const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
-  // a lane's place in a transposing read: of every 16 lanes, lane s names row s / 4 and columns 4 (s % 4).. and gets
-  // column s of the four rows
-  const int tr_row = (lane >> 5) * 8 + ((lane & 15) >> 2), tr_col = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
 
-  for (int64_t t0 = begin; t0 < end; t0 += BK) {
-    __syncthreads();
+  // step k, one of the fast ones, from memory into registers
+  auto load = [&](int64_t k, AR (&ra)[8], BR (&rb)[8], uint32_t (&re)[8]) __attribute__((always_inline)) {
+    const int64_t t0 = begin + k * BK;
+    const unsigned char* dy = static_cast<const unsigned char*>(a.dy) + (t0 * a.lddy + o0) * (int64_t)sizeof(T);
+    const unsigned char* codes = reinterpret_cast<const unsigned char*>(a.codes) + t0 * pitch + i0;
+    const unsigned char* exponents = a.exponents + t0 * epitch + (i0 >> 5);
 #pragma unroll
-    for (int n = 0; n < A_N; ++n) {
-      const int64_t t = t0 + ar + n * A_ROWS;
-      float v[8];
-      fa_load8(static_cast<const T*>(a.dy) + t * a.lddy + o0 + ac, t < end ? a.outputs - o0 - ac : 0, v);
+    for (int j = 0; j < 8; ++j) {
+      ra[j] = load_words<S::AW>(dy + j * a.lddy * (int64_t)sizeof(T) + a_off);
+      rb[j] = *reinterpret_cast<const BR*>(codes + j * pitch + b_off);
+      re[j] = (exponents + j * epitch)[e_off];
+    }
+  };
+  // any step; rows past the end are zero, and nothing that is not there is read
+  auto load_edge = [&](int64_t k, AR (&ra)[8], BR (&rb)[8], uint32_t (&re)[8]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[e] += v[e];
-      unsigned char* at = &la[0][(ar + n * A_ROWS) * AP + ac * 2];
-      if constexpr (PLANES == 1) {
-        uint4 u;
-        u.x = upper_halves(__float_as_uint(v[0]), __float_as_uint(v[1]));
-        u.y = upper_halves(__float_as_uint(v[2]), __float_as_uint(v[3]));
-        u.z = upper_halves(__float_as_uint(v[4]), __float_as_uint(v[5]));
-        u.w = upper_halves(__float_as_uint(v[6]), __float_as_uint(v[7]));
-        *reinterpret_cast<uint4*>(at) = u;
-      } else {
-        uint32_t piece[3][8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) split3(v[e], &piece[0][e], &piece[1][e], &piece[2][e]);
-#pragma unroll
-        for (int q = 0; q < 3; ++q)
-          *reinterpret_cast<uint4*>(at + q * (BK * AP)) =
-              make_uint4(upper_halves(piece[q][0], piece[q][1]), upper_halves(piece[q][2], piece[q][3]),
-                         upper_halves(piece[q][4], piece[q][5]), upper_halves(piece[q][6], piece[q][7]));
+    for (int j = 0; j < 8; ++j) {
+      const int64_t ta = begin + k * BK + a_piece * 8 + j, tb = begin + k * BK + b_piece * 8 + j;
+      ra[j] = load_some<S::AW>(static_cast<const T*>(a.dy) + ta * a.lddy + o0 + a_col, ta < end ? a.outputs - o0 - a_col : 0);
+      rb[j] = BR{};
+      re[j] = 0u;
+      if (tb < end) {
+        rb[j] = *reinterpret_cast<const BR*>(a.codes + tb * pitch + i0 + b_safe);
+        re[j] = a.exponents[tb * epitch + ((i0 + b_safe) >> 5)];
       }
     }
+  };
+  // Places in LDS as a few addresses of the lane and constants.  With column j = 8 g + r, swizzle(j) = swizzle(8 g) ^ (r / 2):
+  // a unit's column 8 g + r is written at put[r / 2] + r ROW.  With j = j0 + 32 m, swizzle(j) = swizzle(j0) ^ 4 (m % 2):
+  // piece 2 kk + lane / 32 of it is read at get[kk ^ 2 (m % 2)] + 32 m ROW.  Of the two wavefronts that share their
+  // outputs, each adds up one half of them, the half that it takes first: its results are in the order turned by `turn`.
+  uint32_t put_a[4], put_b[4], get_first[4], get_last[4], get_b[4];
+  const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
+  const int turn = FM > 1 ? (wave & 1) * HM : 0;
 #pragma unroll
-    for (int n = 0; n < B_N; ++n) {
-      const int64_t t = t0 + br + n * B_ROWS;
-      uint4 codes = make_uint4(0u, 0u, 0u, 0u);
-      float scale = 0.f;
-      if (t < end && i0 + bc < pitch) {
-        codes = *reinterpret_cast<const uint4*>(a.codes + t * pitch + i0 + bc);
-        scale = fa_block_scale(a.exponents[t * epitch + ((i0 + bc) >> 5)]);
-      }
-      float v[16];
-      fa_values8(make_uint2(codes.x, codes.y), scale, v);
-      fa_values8(make_uint2(codes.z, codes.w), scale, v + 8);
-      uint32_t u[8];
+  for (int y = 0; y < 4; ++y) {
+    put_a[y] = a_col * S::ROW + ((a_piece ^ swizzle(a_col) ^ y) << 4);
+    put_b[y] = 2 * S::A_BYTES + b_col * S::ROW + ((b_piece ^ swizzle(b_col) ^ y) << 4);
+    const int jf = wm + 32 * turn + (lane & 31), jl = wm + 32 * (HM - turn) + (lane & 31), jb = wn + (lane & 31);
+    const int piece = (lane >> 5) ^ (2 * y);
+    get_first[y] = jf * S::ROW + ((piece ^ swizzle(jf)) << 4);
+    get_last[y] = jl * S::ROW + ((piece ^ swizzle(jl)) << 4);
+    get_b[y] = 2 * S::A_BYTES + jb * S::ROW + ((piece ^ swizzle(jb)) << 4);
+  }
+  // a quarter (of four) of a step's registers into LDS
+  auto stage = [&](int quarter, int half, const AR (&ra)[8], const BR (&rb)[8],
+                   const uint32_t (&re)[8]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) u[e] = upper_halves(__float_as_uint(v[2 * e]), __float_as_uint(v[2 * e + 1]));
-      uint4* at = reinterpret_cast<uint4*>(&lb[(br + n * B_ROWS) * BP + bc * 2]);
-      at[0] = make_uint4(u[0], u[1], u[2], u[3]);
-      at[1] = make_uint4(u[4], u[5], u[6], u[7]);
-    }
-    __syncthreads();
+    for (int c = quarter * AC / 4; c < (quarter + 1) * AC / 4; ++c) {
+      unsigned char* at = lds + put_a[c >> 1] + (half * S::A_BYTES + c * S::ROW);
+      fa_u32x4 u[3];
 #pragma unroll
-    for (int kk = 0; kk < BK; kk += 16) {
-      bf16x8 fb[FN];
-#pragma unroll
-      for (int n = 0; n < FN; ++n) {
-        const unsigned char* at = &lb[(kk + tr_row) * BP + (wn + 32 * n + tr_col) * 2];
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * BP));
-        fb[n] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-      }
-#pragma unroll
-      for (int q = PLANES - 1; q >= 0; --q)
-#pragma unroll
-        for (int m = 0; m < FM; ++m) {
-          const unsigned char* at = &la[q][(kk + tr_row) * AP + (wm + 32 * m + tr_col) * 2];
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * AP));
-          const bf16x8 fa = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-          for (int n = 0; n < FN; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, fb[n], acc[m][n], 0, 0, 0);
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (S::PLANES == 1) {
+          u[0][e] = __builtin_amdgcn_perm(ra[2 * e + 1][c >> 1], ra[2 * e][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
+        } else {
+          uint32_t h0, m0, l0, h1, m1, l1;
+          split3(__uint_as_float(ra[2 * e][c]), &h0, &m0, &l0);
+          split3(__uint_as_float(ra[2 * e + 1][c]), &h1, &m1, &l1);
+          u[0][e] = upper_halves(h0, h1);
+          u[1][e] = upper_halves(m0, m1);
+          u[2][e] = upper_halves(l0, l1);
         }
+      }
+#pragma unroll
+      for (int q = 0; q < S::PLANES; ++q) *reinterpret_cast<fa_u32x4*>(at + q * (BM * S::ROW)) = u[q];
+    }
+#pragma unroll
+    for (int c = quarter * S::BC / 4; c < (quarter + 1) * S::BC / 4; ++c) {
+      fa_u32x4 u;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float v0 = (float)(int8_t)(rb[2 * e][c >> 2] >> (8 * (c & 3))) * fa_block_scale(re[2 * e]);
+        const float v1 = (float)(int8_t)(rb[2 * e + 1][c >> 2] >> (8 * (c & 3))) * fa_block_scale(re[2 * e + 1]);
+        u[e] = upper_halves(__float_as_uint(v0), __float_as_uint(v1));
+      }
+      *reinterpret_cast<fa_u32x4*>(lds + put_b[c >> 1] + (half * S::B_BYTES + c * S::ROW)) = u;
+    }
+  };
+  // the operands of 16 rows of a step, and their products
+  auto fetch = [&](int half, int kk, bf16x8 (&fa)[S::PLANES][FM], bf16x8 (&fb)[FN]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int n = 0; n < FN; ++n)
+      fb[n] = *reinterpret_cast<const bf16x8*>(lds + get_b[kk ^ (2 * (n & 1))] + (half * S::B_BYTES + 32 * n * S::ROW));
+#pragma unroll
+    for (int q = 0; q < S::PLANES; ++q)
+#pragma unroll
+      for (int m = 0; m < FM; ++m) {
+        const int mm = m < HM ? m : m - HM;
+        const uint32_t at = m < HM ? get_first[kk ^ (2 * (mm & 1))] : get_last[kk ^ (2 * (mm & 1))];
+        fa[q][m] = *reinterpret_cast<const bf16x8*>(lds + at + (half * S::A_BYTES + 32 * mm * S::ROW + q * (BM * S::ROW)));
+      }
+  };
+  auto multiply = [&](const bf16x8 (&fa)[S::PLANES][FM], const bf16x8 (&fb)[FN]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int q = S::PLANES - 1; q >= 0; --q)
+#pragma unroll
+      for (int m = 0; m < FM; ++m) {
+        if (m < HM) sum[m] = add8(fa[q][m], sum[m]);
+#pragma unroll
+        for (int n = 0; n < FN; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[q][m], fb[n], acc[m][n], 0, 0, 0);
+      }
+  };
+  // the registers of a step are what they were loaded as until here (the compiler would convert them where they arrive,
+  // a step early, and has no registers for that)
+  auto here = [&](AR (&ra)[8], BR (&rb)[8], uint32_t (&re)[8]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      asm volatile("" : "+v"(ra[j]), "+v"(re[j]));
+      if constexpr (S::BW == 1) {
+        uint32_t u = rb[j][0];
+        asm volatile("" : "+v"(u));
+        rb[j][0] = u;
+      } else {
+        asm volatile("" : "+v"(rb[j]));
+      }
+    }
+  };
+  bf16x8 fa[2][S::PLANES][FM], fb[2][FN];
+  if (fast > 0) {
+    // (past the last fast step the last one is loaded again, and goes where nobody reads it)
+    load(0, raw_a[0], raw_b[0], raw_e[0]);
+    load(min((int64_t)1, fast - 1), raw_a[1], raw_b[1], raw_e[1]);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) stage(q, 0, raw_a[0], raw_b[0], raw_e[0]);
+    lds_barrier();
+    int64_t k = 0;
+    for (; k + 1 < fast; k += 2) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        fetch(half, 0, fa[0], fb[0]);
+        load(min(k + half + 2, fast - 1), raw_a[half], raw_b[half], raw_e[half]);
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          if (kk + 1 < KK) fetch(half, kk + 1, fa[(kk + 1) & 1], fb[(kk + 1) & 1]);
+          multiply(fa[kk & 1], fb[kk & 1]);
+          if (kk == 0) here(raw_a[1 - half], raw_b[1 - half], raw_e[1 - half]);
+          stage(kk, 1 - half, raw_a[1 - half], raw_b[1 - half], raw_e[1 - half]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        lds_barrier();
+      }
+    }
+    if (k < fast) {
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        fetch(0, kk, fa[0], fb[0]);
+        multiply(fa[0], fb[0]);
+      }
+      lds_barrier();
     }
   }
-  // b_w: the threads that brought in the same outputs, in their order
-  __syncthreads();
-  float* part = reinterpret_cast<float*>(lb);
-  static_assert(A_ROWS * BM * 4 <= BK * BP, "the column sums fit");
+  for (int64_t k = fast; k < steps; ++k) {
+    load_edge(k, raw_a[0], raw_b[0], raw_e[0]);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) part[ar * BM + ac + e] = sum[e];
-  __syncthreads();
-  if (tid < BM) {
-    float s = 0.f;
+    for (int q = 0; q < 4; ++q) stage(q, 0, raw_a[0], raw_b[0], raw_e[0]);
+    lds_barrier();
 #pragma unroll
-    for (int r = 0; r < A_ROWS; ++r) s += part[r * BM + tid];
-    bias[tid] = s;
+    for (int kk = 0; kk < KK; ++kk) {
+      fetch(0, kk, fa[0], fb[0]);
+      multiply(fa[0], fb[0]);
+    }
+    lds_barrier();
+  }
+  // b_w: the lanes l and l + 32 have the two halves of every eight rows
+  float* bias = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int m = 0; m < HM; ++m) {
+    sum[m] += __shfl_xor(sum[m], 32);
+    if (lane < 32 && (FM > 1 || wn == 0)) bias[wm + 32 * (m + turn) + lane] = sum[m];
   }
   __syncthreads();
   const int64_t OI = (int64_t)a.outputs * a.features;
@@ -183,7 +346,7 @@ __global__ __launch_bounds__(kThreads) void fa_linear_grad_kernel(fa_linear_grad
       for (int m = 0; m < FM; ++m)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int o = o0 + wm + 32 * m + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
+          const int o = o0 + wm + 32 * (m < HM ? m + turn : m - turn) + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
           if (i < a.features && o < a.outputs) out[(int64_t)o * a.features + i] = acc[m][n][r];
         }
     }
@@ -206,7 +369,7 @@ __global__ __launch_bounds__(kThreads) void fa_linear_grad_kernel(fa_linear_grad
     for (int m = 0; m < FM; ++m)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int ol = wm + 32 * m + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
+        const int ol = wm + 32 * (m < HM ? m + turn : m - turn) + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
         if (i < a.features && o0 + ol < a.outputs) {
           const float v = a.gamma ? gamma * acc[m][n][r] + beta * bias[ol] : acc[m][n][r];
           const int64_t at = w * a.lddweight + (int64_t)(o0 + ol) * a.features + i;
@@ -248,30 +411,48 @@ __global__ __launch_bounds__(kThreads) void fa_linear_grad_join_kernel(fa_linear
 }
 
 namespace {
-constexpr int kBM = 128, kBN = 128, kBK = 32;
-}
 
-int fa_linear_grad_splits(const fa_row_blocks& b, int features, int outputs, int dtype) {
-  (void)dtype;
+// The two tiles of either type.  (outputs, features)
+constexpr int kWide[2][2] = {{128, 256}, {256, 256}}, kNarrow[2][2] = {{64, 128}, {128, 128}};
+
+struct plan {
+  bool wide;
+  int splits;
+  int64_t tiles;   // of one worker
+};
+
+plan plan_of(const fa_row_blocks& b, int features, int outputs, int dtype) {
+  const int bf16 = dtype == FA_BF16;
   int64_t most = 0;
   for (int w = 0; w < b.p; ++w) most = b.row0[w + 1] - b.row0[w] > most ? b.row0[w + 1] - b.row0[w] : most;
-  const int64_t tiles = (int64_t)b.p * ((outputs + kBM - 1) / kBM) * ((features + kBN - 1) / kBN);
-  int64_t s = 512 / tiles;
+  auto tiles = [&](const int* t) { return (int64_t)((outputs + t[0] - 1) / t[0]) * ((features + t[1] - 1) / t[1]); };
+  plan c;
+  c.wide = tiles(kWide[bf16]) * b.p >= 200;
+  c.tiles = tiles(c.wide ? kWide[bf16] : kNarrow[bf16]);
+  int64_t s = 512 / (c.tiles * b.p);
   if (s > most / 256) s = most / 256;
-  return s < 1 ? 1 : (int)s;
+  c.splits = s < 1 ? 1 : (int)s;
+  return c;
 }
 
-size_t fa_linear_grad_partials(const fa_row_blocks& b, int features, int outputs, int splits) {
+}  // namespace
+
+size_t fa_linear_grad_partials(const fa_row_blocks& b, int features, int outputs, int dtype) {
+  const int splits = plan_of(b, features, outputs, dtype).splits;
   return splits > 1 ? sizeof(float) * (size_t)b.p * splits * ((size_t)outputs * features + outputs) : 0;
 }
 
-hipError_t fa_launch_linear_grad(const fa_linear_grad_args& a, int dtype, hipStream_t st) {
-  const int64_t tiles = (int64_t)((a.outputs + kBM - 1) / kBM) * ((a.features + kBN - 1) / kBN);
-  const dim3 grid((unsigned)(tiles * a.blocks.p * a.splits));
-  if (dtype == FA_F32)
-    hipLaunchKernelGGL((fa_linear_grad_kernel<float, kBM, kBN, kBK>), grid, dim3(kThreads), 0, st, a);
-  else
-    hipLaunchKernelGGL((fa_linear_grad_kernel<fa_bf16, kBM, kBN, kBK>), grid, dim3(kThreads), 0, st, a);
+hipError_t fa_launch_linear_grad(fa_linear_grad_args a, int dtype, hipStream_t st) {
+  const plan c = plan_of(a.blocks, a.features, a.outputs, dtype);
+  a.splits = c.splits;
+  const dim3 grid((unsigned)(c.tiles * a.blocks.p * c.splits));
+  if (dtype == FA_F32) {
+    if (c.wide) hipLaunchKernelGGL((fa_linear_grad_kernel<float, 128, 256, 64>), grid, dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL((fa_linear_grad_kernel<float, 64, 128, 64>), grid, dim3(kThreads), 0, st, a);
+  } else {
+    if (c.wide) hipLaunchKernelGGL((fa_linear_grad_kernel<fa_bf16, 256, 256, 64>), grid, dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL((fa_linear_grad_kernel<fa_bf16, 128, 128, 64>), grid, dim3(kThreads), 0, st, a);
+  }
   if (a.splits > 1) {
     int64_t blocks = ((int64_t)a.outputs * a.features + a.outputs + kThreads - 1) / kThreads;
     if (blocks > 2048) blocks = 2048;
