@@ -69,6 +69,21 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// The tile of workgroup b of n.  Workgroups go to the eight dies in turn, and every die has its own L2: each gets one run of
+// consecutive tiles, in which bands of four rows of tiles are walked column by column, so that the 32 workgroups of a die
+// share four strips of dY and eight of codes.
+struct place {
+  int group, to, ti;   // which worker and split, which tile
+};
+__device__ __forceinline__ place place_of(uint32_t b, uint32_t n, int tiles_o, int tiles_i) {
+  const uint32_t die = b % 8, whole = n / 8, more = n % 8;
+  const uint32_t id = die * whole + min(die, more) + b / 8;
+  const uint32_t per_group = (uint32_t)tiles_o * tiles_i, in = id % per_group;
+  const uint32_t band = in / (4 * tiles_i), rest = in - band * 4 * tiles_i;
+  const uint32_t rows = min(4u, tiles_o - 4 * band);
+  return {(int)(id / per_group), (int)(4 * band + rest % rows), (int)(rest / rows)};
+}
+
 template <int N>
 using words = uint32_t __attribute__((ext_vector_type(N)));
 
@@ -77,6 +92,15 @@ __device__ __forceinline__ words<N> load_words(const unsigned char* p) {   // at
   words<N> u;
   __builtin_memcpy(&u, p, sizeof(u));
   return u;
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const unsigned char* p) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(p), 0, 0x7fffffff, 0x00020000);
+}
+template <int N>
+__device__ __forceinline__ words<N> buffer_words(__amdgpu_buffer_rsrc_t r, uint32_t lane, int row) {
+  if constexpr (N == 4) return __builtin_bit_cast(words<4>, __builtin_amdgcn_raw_buffer_load_b128(r, lane, row, 0));
+  else if constexpr (N == 2) return __builtin_bit_cast(words<2>, __builtin_amdgcn_raw_buffer_load_b64(r, lane, row, 0));
+  else return __builtin_bit_cast(words<1>, __builtin_amdgcn_raw_buffer_load_b32(r, lane, row, 0));
 }
 // a unit's row of dY of which the first `valid` elements exist, zeros behind them
 template <int N>
@@ -96,6 +120,24 @@ __device__ __forceinline__ words<N> load_some(const float* p, int valid) {
   for (int e = 0; e < N; ++e)
     if (e < valid) u[e] = __float_as_uint(p[e]);
   return u;
+}
+
+// A wavefront issues in order: what is not a product goes between the products, a few instructions behind each, and costs
+// nothing there.  PRODUCTS matrix instructions, READS and WRITES of LDS and the vector instructions of a region.
+template <int PRODUCTS, int READS, int WRITES, int VECTOR, int I = 0>
+__device__ __forceinline__ void interleave() {
+  if constexpr (I < PRODUCTS) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                                        // a product
+    if constexpr (2 * I < READS) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    __builtin_amdgcn_sched_group_barrier(0x020, 2, 0);                                        // loads from memory
+    constexpr int V = VECTOR * (I + 1) / PRODUCTS - VECTOR * I / PRODUCTS;
+    if constexpr (V > 0) __builtin_amdgcn_sched_group_barrier(0x002, V, 0);
+    // (writes behind all reads: nothing tells the compiler that they go to the other half)
+    constexpr int FROM = READS / 2, OVER = PRODUCTS - FROM > 0 ? PRODUCTS - FROM : 1, J = I - FROM;
+    constexpr int W = J < 0 ? 0 : WRITES * (J + 1) / OVER - WRITES * J / OVER;
+    if constexpr (W > 0) __builtin_amdgcn_sched_group_barrier(0x200, W, 0);
+    interleave<PRODUCTS, READS, WRITES, VECTOR, I + 1>();
+  }
 }
 
 // s + the sum of eight bf16 values, in fp32
@@ -118,13 +160,9 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
   __shared__ __attribute__((aligned(16))) unsigned char lds[2 * (S::A_BYTES + S::B_BYTES)];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int tiles_o = (a.outputs + BM - 1) / BM, tiles_i = (a.features + BN - 1) / BN;
-  int64_t id = blockIdx.x;
-  const int ti = (int)(id % tiles_i);
-  id /= tiles_i;
-  const int to = (int)(id % tiles_o);
-  id /= tiles_o;
-  const int split = (int)(id % a.splits), w = (int)(id / a.splits);
-  const int o0 = to * BM, i0 = ti * BN;
+  const place at = place_of(blockIdx.x, gridDim.x, tiles_o, tiles_i);
+  const int split = at.group % a.splits, w = at.group / a.splits;
+  const int o0 = at.to * BM, i0 = at.ti * BN;
   // this split's rows: whole steps of BK rows
   const int64_t all = a.blocks.row0[w + 1] - a.blocks.row0[w];
   const int64_t steps_all = (all + BK - 1) / BK, per = (steps_all + a.splits - 1) / a.splits;
@@ -141,7 +179,7 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
   const int b_col = tid % (BN / S::BC) * S::BC, b_piece = tid / (BN / S::BC);
   const int64_t over = (AC - a.outputs % AC) % AC;        // elements of the last unit past the last column
   const int64_t reach = a.blocks.row0[a.blocks.p] - (over + a.lddy - 1) / a.lddy;
-  const int64_t fast = a.lddy < (1 << 24) && min(end, reach) > begin ? (min(end, reach) - begin) / BK : 0;
+  const int64_t fast = a.lddy < (1 << 22) && min(end, reach) > begin ? (min(end, reach) - begin) / BK : 0;
   const int64_t steps = (end - begin + BK - 1) / BK;
   const uint32_t a_off = (uint32_t)((int64_t)a_piece * 8 * a.lddy + (o0 + a_col < a.outputs ? a_col : 0)) * (uint32_t)sizeof(T);
   const int b_safe = i0 + b_col < pitch ? b_col : 0;
@@ -163,18 +201,26 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[m][n][r] = 0.f;
 
-  // step k, one of the fast ones, from memory into registers
-  auto load = [&](int64_t k, AR (&ra)[8], BR (&rb)[8], uint32_t (&re)[8]) __attribute__((always_inline)) {
-    const int64_t t0 = begin + k * BK;
-    const unsigned char* dy = static_cast<const unsigned char*>(a.dy) + (t0 * a.lddy + o0) * (int64_t)sizeof(T);
-    const unsigned char* codes = reinterpret_cast<const unsigned char*>(a.codes) + t0 * pitch + i0;
-    const unsigned char* exponents = a.exponents + t0 * epitch + (i0 >> 5);
+  // One of the fast steps from memory into registers, and on to the next.  (Buffer loads: a lane's place in the step, a row's
+  // distance and the step's own address are three operands of the instruction, none of them is added up for a load.)
+  const unsigned char* at_dy = static_cast<const unsigned char*>(a.dy) + (begin * a.lddy + o0) * (int64_t)sizeof(T);
+  const unsigned char* at_codes = reinterpret_cast<const unsigned char*>(a.codes) + begin * pitch + i0;
+  const unsigned char* at_exponents = a.exponents + begin * epitch + (i0 >> 5);
+  const int row_dy = (int)a.lddy * (int)sizeof(T), row_codes = (int)pitch, row_exponents = (int)epitch;
+  int64_t ahead = fast - 1;                               // steps to go on by: the last one is loaded again and again
+  auto load = [&](AR (&ra)[8], BR (&rb)[8], uint32_t (&re)[8]) __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t dy = buffer(at_dy), codes = buffer(at_codes), exponents = buffer(at_exponents);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      ra[j] = load_words<S::AW>(dy + j * a.lddy * (int64_t)sizeof(T) + a_off);
-      rb[j] = *reinterpret_cast<const BR*>(codes + j * pitch + b_off);
-      re[j] = (exponents + j * epitch)[e_off];
+      ra[j] = buffer_words<S::AW>(dy, a_off, j * row_dy);
+      rb[j] = buffer_words<S::BW>(codes, b_off, j * row_codes);
+      re[j] = __builtin_amdgcn_raw_buffer_load_b8(exponents, e_off, j * row_exponents, 0);
     }
+    const int on = ahead > 0 ? BK : 0;
+    at_dy += (int64_t)on * row_dy;
+    at_codes += (int64_t)on * row_codes;
+    at_exponents += (int64_t)on * row_exponents;
+    --ahead;
   };
   // any step; rows past the end are zero, and nothing that is not there is read
   auto load_edge = [&](int64_t k, AR (&ra)[8], BR (&rb)[8], uint32_t (&re)[8]) __attribute__((always_inline)) {
@@ -271,21 +317,22 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
   auto here = [&](AR (&ra)[8], BR (&rb)[8], uint32_t (&re)[8]) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      asm volatile("" : "+v"(ra[j]), "+v"(re[j]));
+      asm("" : "+v"(ra[j]), "+v"(re[j]));
       if constexpr (S::BW == 1) {
         uint32_t u = rb[j][0];
-        asm volatile("" : "+v"(u));
+        asm("" : "+v"(u));
         rb[j][0] = u;
       } else {
-        asm volatile("" : "+v"(rb[j]));
+        asm("" : "+v"(rb[j]));
       }
     }
   };
+  // vector instructions of a quarter: 20 for a column of codes, 4 or 88 for one of dY, 4 for each column sum
+  constexpr int kVector = S::BC / 4 * 20 + S::AC * (S::PLANES == 1 ? 4 : 88) / 4 + S::PLANES * HM * 4;
   bf16x8 fa[2][S::PLANES][FM], fb[2][FN];
   if (fast > 0) {
-    // (past the last fast step the last one is loaded again, and goes where nobody reads it)
-    load(0, raw_a[0], raw_b[0], raw_e[0]);
-    load(min((int64_t)1, fast - 1), raw_a[1], raw_b[1], raw_e[1]);
+    load(raw_a[0], raw_b[0], raw_e[0]);
+    load(raw_a[1], raw_b[1], raw_e[1]);
 #pragma unroll
     for (int q = 0; q < 4; ++q) stage(q, 0, raw_a[0], raw_b[0], raw_e[0]);
     lds_barrier();
@@ -294,13 +341,14 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         fetch(half, 0, fa[0], fb[0]);
-        load(min(k + half + 2, fast - 1), raw_a[half], raw_b[half], raw_e[half]);
+        load(raw_a[half], raw_b[half], raw_e[half]);
+        here(raw_a[1 - half], raw_b[1 - half], raw_e[1 - half]);
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
           if (kk + 1 < KK) fetch(half, kk + 1, fa[(kk + 1) & 1], fb[(kk + 1) & 1]);
           multiply(fa[kk & 1], fb[kk & 1]);
-          if (kk == 0) here(raw_a[1 - half], raw_b[1 - half], raw_e[1 - half]);
           stage(kk, 1 - half, raw_a[1 - half], raw_b[1 - half], raw_e[1 - half]);
+          interleave<S::PLANES * FM * FN, S::PLANES * FM + FN, (S::PLANES * S::AC + S::BC) / 4, kVector>();
           __builtin_amdgcn_sched_barrier(0);
         }
         lds_barrier();
@@ -338,7 +386,7 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
   const int64_t OI = (int64_t)a.outputs * a.features;
   if (a.splits > 1) {
     float* out = a.partials + ((int64_t)w * a.splits + split) * (OI + a.outputs);
-    if (ti == 0 && tid < BM && o0 + tid < a.outputs) out[OI + o0 + tid] = bias[tid];
+    if (at.ti == 0 && tid < BM && o0 + tid < a.outputs) out[OI + o0 + tid] = bias[tid];
 #pragma unroll
     for (int n = 0; n < FN; ++n) {
       const int i = i0 + wn + 32 * n + (lane & 31);
@@ -352,7 +400,7 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
     }
     return;
   }
-  if (a.dbias && ti == 0 && tid < BM && o0 + tid < a.outputs) {
+  if (a.dbias && at.ti == 0 && tid < BM && o0 + tid < a.outputs) {
     const int64_t at = w * a.lddbias + o0 + tid;
     if (a.grad_bf16) fa_store1(static_cast<fa_bf16*>(a.dbias) + at, bias[tid]);
     else fa_store1(static_cast<float*>(a.dbias) + at, bias[tid]);
