@@ -69,6 +69,11 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // The tile of workgroup b of n.  Workgroups go to the eight dies in turn, and every die has its own L2: each gets one run of
 // consecutive tiles, in which bands of four rows of tiles are walked column by column, so that the 32 workgroups of a die
 // share four strips of dY and eight of codes.
@@ -384,47 +389,52 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
   }
   __syncthreads();
   const int64_t OI = (int64_t)a.outputs * a.features;
-  if (a.splits > 1) {
-    float* out = a.partials + ((int64_t)w * a.splits + split) * (OI + a.outputs);
-    if (at.ti == 0 && tid < BM && o0 + tid < a.outputs) out[OI + o0 + tid] = bias[tid];
-#pragma unroll
-    for (int n = 0; n < FN; ++n) {
-      const int i = i0 + wn + 32 * n + (lane & 31);
-#pragma unroll
-      for (int m = 0; m < FM; ++m)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int o = o0 + wm + 32 * (m < HM ? m + turn : m - turn) + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
-          if (i < a.features && o < a.outputs) out[(int64_t)o * a.features + i] = acc[m][n][r];
-        }
-    }
-    return;
+  float* part = a.splits > 1 ? a.partials + ((int64_t)w * a.splits + split) * (OI + a.outputs) : nullptr;
+  if (at.ti == 0 && tid < BM && o0 + tid < a.outputs) {
+    if (part) part[OI + o0 + tid] = bias[tid];
+    else if (a.dbias && a.grad_bf16) fa_store1(static_cast<fa_bf16*>(a.dbias) + w * a.lddbias + o0 + tid, bias[tid]);
+    else if (a.dbias) static_cast<float*>(a.dbias)[w * a.lddbias + o0 + tid] = bias[tid];
   }
-  if (a.dbias && at.ti == 0 && tid < BM && o0 + tid < a.outputs) {
-    const int64_t at = w * a.lddbias + o0 + tid;
-    if (a.grad_bf16) fa_store1(static_cast<fa_bf16*>(a.dbias) + at, bias[tid]);
-    else fa_store1(static_cast<float*>(a.dbias) + at, bias[tid]);
+  // A lane of a result block has single features of eight outputs; through LDS it gets eight features of one, and the
+  // gradient is written 16 bytes or more a lane.  (Rows of a block are 32 bytes apart from whole banks: the two rows
+  // that one store puts down, four apart, meet on no bank.)
+  constexpr int PITCH = BN / 2 + 8, LANES = BN / 16, ROWS = 64 / LANES;
+  static_assert(BM * 4 + 4 * 32 * PITCH * 4 <= (int)sizeof(lds), "a block of every wavefront fits");
+  float* block = bias + BM + wave * 32 * PITCH;
+  const int i = i0 + wn + lane % LANES * 8, valid = a.features - i;
+  float gamma[8], beta[8];
+  const bool affine = a.gamma && !part;
+  if (affine) {
+    fa_load8_param(a.gamma, a.param_bf16, i, valid, gamma);
+    fa_load8_param(a.beta, a.param_bf16, i, valid, beta);
   }
 #pragma unroll
-  for (int n = 0; n < FN; ++n) {
-    const int i = i0 + wn + 32 * n + (lane & 31);
-    float gamma = 1.f, beta = 0.f;
-    if (a.gamma && i < a.features) {
-      gamma = a.param_bf16 ? fa_load1(static_cast<const fa_bf16*>(a.gamma) + i) : static_cast<const float*>(a.gamma)[i];
-      beta = a.param_bf16 ? fa_load1(static_cast<const fa_bf16*>(a.beta) + i) : static_cast<const float*>(a.beta)[i];
-    }
+  for (int m = 0; m < FM; ++m) {
+    const int o_block = wm + 32 * (m < HM ? m + turn : m - turn);
+    wave_fence();
 #pragma unroll
-    for (int m = 0; m < FM; ++m)
+    for (int n = 0; n < FN; ++n)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int ol = wm + 32 * (m < HM ? m + turn : m - turn) + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
-        if (i < a.features && o0 + ol < a.outputs) {
-          const float v = a.gamma ? gamma * acc[m][n][r] + beta * bias[ol] : acc[m][n][r];
-          const int64_t at = w * a.lddweight + (int64_t)(o0 + ol) * a.features + i;
-          if (a.grad_bf16) fa_store1(static_cast<fa_bf16*>(a.dweight) + at, v);
-          else fa_store1(static_cast<float*>(a.dweight) + at, v);
+      for (int r = 0; r < 16; ++r)
+        block[((r & 3) + 8 * (r >> 2) + 4 * (lane >> 5)) * PITCH + 32 * n + (lane & 31)] = acc[m][n][r];
+    wave_fence();
+#pragma unroll
+    for (int row = 0; row < 32; row += ROWS) {
+      const int in = row + lane / LANES, o = o0 + o_block + in;
+      float v[8];
+      fa_load8_whole(block + in * PITCH + lane % LANES * 8, v);
+      if (o < a.outputs) {
+        const int64_t to = (int64_t)o * a.features + i;
+        if (affine) {
+          const float b = bias[o_block + in];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = gamma[e] * v[e] + beta[e] * b;
         }
+        if (part) fa_store8(part + to, valid, v);
+        else if (a.grad_bf16) fa_store8(static_cast<fa_bf16*>(a.dweight) + w * a.lddweight + to, valid, v);
+        else fa_store8(static_cast<float*>(a.dweight) + w * a.lddweight + to, valid, v);
       }
+    }
   }
 }
 
