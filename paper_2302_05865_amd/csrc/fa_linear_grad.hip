@@ -58,7 +58,7 @@ struct tile {
   static constexpr int AC = BM * PIECES / kThreads, BC = BN * PIECES / kThreads;
   static constexpr int AW = AC * (int)sizeof(T) / 4, BW = BC / 4;           // dwords of a row of it
   static_assert((AW == 2 || AW == 4) && (BW == 1 || BW == 2), "loads of 8 or 16, and of 4 or 8 bytes");
-  static_assert(PIECES == 8, "swizzle() is for eight pieces");
+  static_assert(BK == 64 && PIECES == 8, "swizzle() is for eight pieces");
 };
 
 __device__ __forceinline__ int swizzle(int column) { return ((column >> 1) ^ (column >> 3)) & 7; }
@@ -336,27 +336,38 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
   constexpr int kVector = S::BC / 4 * 20 + S::AC * (S::PLANES == 1 ? 4 : 88) / 4 + S::PLANES * HM * 4;
   bf16x8 fa[2][S::PLANES][FM], fb[2][FN];
   if (fast > 0) {
+    // A step k in half k % 2 of LDS takes four regions of 16 rows.  In the first three the last quarters of step k + 1 are
+    // put down; behind the barrier everyone is done reading step k and step k + 1 is complete, so that the fourth region
+    // fetches the first operands of step k + 1, puts down the first quarter of step k + 2 where step k was, and sends
+    // for step k + 3.  (Past the last fast step the last one comes again, and nobody uses it.)
     load(raw_a[0], raw_b[0], raw_e[0]);
     load(raw_a[1], raw_b[1], raw_e[1]);
 #pragma unroll
     for (int q = 0; q < 4; ++q) stage(q, 0, raw_a[0], raw_b[0], raw_e[0]);
+    load(raw_a[0], raw_b[0], raw_e[0]);
     lds_barrier();
+    fetch(0, 0, fa[0], fb[0]);
+    stage(0, 1, raw_a[1], raw_b[1], raw_e[1]);
     int64_t k = 0;
     for (; k + 1 < fast; k += 2) {
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        fetch(half, 0, fa[0], fb[0]);
-        load(raw_a[half], raw_b[half], raw_e[half]);
-        here(raw_a[1 - half], raw_b[1 - half], raw_e[1 - half]);
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
-          if (kk + 1 < KK) fetch(half, kk + 1, fa[(kk + 1) & 1], fb[(kk + 1) & 1]);
+          if (kk + 1 < KK) {
+            fetch(half, kk + 1, fa[(kk + 1) & 1], fb[(kk + 1) & 1]);
+          } else {
+            lds_barrier();
+            fetch(1 - half, 0, fa[0], fb[0]);
+            load(raw_a[1 - half], raw_b[1 - half], raw_e[1 - half]);
+            here(raw_a[half], raw_b[half], raw_e[half]);
+          }
           multiply(fa[kk & 1], fb[kk & 1]);
-          stage(kk, 1 - half, raw_a[1 - half], raw_b[1 - half], raw_e[1 - half]);
+          if (kk + 1 < KK) stage(kk + 1, 1 - half, raw_a[1 - half], raw_b[1 - half], raw_e[1 - half]);
+          else stage(0, half, raw_a[half], raw_b[half], raw_e[half]);
           interleave<S::PLANES * FM * FN, S::PLANES * FM + FN, (S::PLANES * S::AC + S::BC) / 4, kVector>();
           __builtin_amdgcn_sched_barrier(0);
         }
-        lds_barrier();
       }
     }
     if (k < fast) {
@@ -365,8 +376,8 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
         fetch(0, kk, fa[0], fb[0]);
         multiply(fa[0], fb[0]);
       }
-      lds_barrier();
     }
+    lds_barrier();
   }
   for (int64_t k = fast; k < steps; ++k) {
     load_edge(k, raw_a[0], raw_b[0], raw_e[0]);
