@@ -213,19 +213,22 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
   const unsigned char* at_exponents = a.exponents + begin * epitch + (i0 >> 5);
   const int row_dy = (int)a.lddy * (int)sizeof(T), row_codes = (int)pitch, row_exponents = (int)epitch;
   int64_t ahead = fast - 1;                               // steps to go on by: the last one is loaded again and again
-  auto load = [&](AR (&ra)[8], BR (&rb)[8], uint32_t (&re)[8]) __attribute__((always_inline)) {
+  // (part 0 and 1, half of the rows each; a step's own address goes on behind part 1)
+  auto load = [&](int part, AR (&ra)[8], BR (&rb)[8], uint32_t (&re)[8]) __attribute__((always_inline)) {
     const __amdgpu_buffer_rsrc_t dy = buffer(at_dy), codes = buffer(at_codes), exponents = buffer(at_exponents);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 4 * part; j < 4 * part + 4; ++j) {
       ra[j] = buffer_words<S::AW>(dy, a_off, j * row_dy);
       rb[j] = buffer_words<S::BW>(codes, b_off, j * row_codes);
       re[j] = __builtin_amdgcn_raw_buffer_load_b8(exponents, e_off, j * row_exponents, 0);
     }
-    const int on = ahead > 0 ? BK : 0;
-    at_dy += (int64_t)on * row_dy;
-    at_codes += (int64_t)on * row_codes;
-    at_exponents += (int64_t)on * row_exponents;
-    --ahead;
+    if (part == 1) {
+      const int on = ahead > 0 ? BK : 0;
+      at_dy += (int64_t)on * row_dy;
+      at_codes += (int64_t)on * row_codes;
+      at_exponents += (int64_t)on * row_exponents;
+      --ahead;
+    }
   };
   // any step; rows past the end are zero, and nothing that is not there is read
   auto load_edge = [&](int64_t k, AR (&ra)[8], BR (&rb)[8], uint32_t (&re)[8]) __attribute__((always_inline)) {
@@ -340,11 +343,13 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
     // put down; behind the barrier everyone is done reading step k and step k + 1 is complete, so that the fourth region
     // fetches the first operands of step k + 1, puts down the first quarter of step k + 2 where step k was, and sends
     // for step k + 3.  (Past the last fast step the last one comes again, and nobody uses it.)
-    load(raw_a[0], raw_b[0], raw_e[0]);
-    load(raw_a[1], raw_b[1], raw_e[1]);
+    load(0, raw_a[0], raw_b[0], raw_e[0]);
+    load(1, raw_a[0], raw_b[0], raw_e[0]);
+    load(0, raw_a[1], raw_b[1], raw_e[1]);
+    load(1, raw_a[1], raw_b[1], raw_e[1]);
 #pragma unroll
     for (int q = 0; q < 4; ++q) stage(q, 0, raw_a[0], raw_b[0], raw_e[0]);
-    load(raw_a[0], raw_b[0], raw_e[0]);
+    load(0, raw_a[0], raw_b[0], raw_e[0]);
     lds_barrier();
     fetch(0, 0, fa[0], fb[0]);
     stage(0, 1, raw_a[1], raw_b[1], raw_e[1]);
@@ -356,10 +361,11 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
         for (int kk = 0; kk < KK; ++kk) {
           if (kk + 1 < KK) {
             fetch(half, kk + 1, fa[(kk + 1) & 1], fb[(kk + 1) & 1]);
+            if (kk == 0) load(1, raw_a[half], raw_b[half], raw_e[half]);
           } else {
             lds_barrier();
             fetch(1 - half, 0, fa[0], fb[0]);
-            load(raw_a[1 - half], raw_b[1 - half], raw_e[1 - half]);
+            load(0, raw_a[1 - half], raw_b[1 - half], raw_e[1 - half]);
             here(raw_a[half], raw_b[half], raw_e[half]);
           }
           multiply(fa[kk & 1], fb[kk & 1]);
