@@ -4,11 +4,15 @@
 //   h = dy gamma,  a = sum_j h_j / D,  b = sum_j h_j xhat_j / D,  dx = r (h - a - xhat b) [+ residual]
 //   dgamma_w = sum over the rows of worker w of dy xhat,  dbeta_w = the same of dy
 //
-// A row is held in registers by a team of lanes, eight consecutive features a lane and piece: every row is read once,
-// the variance is that of the centred values, and four neighbouring lanes hold one block of a checkpoint.  Statistics and
-// sums are fp32.
+// Bound by memory: forward reads x and writes y and the checkpoint, backward reads dy and xhat and writes dx, every element
+// once.  A row is held in registers by a team of lanes, eight consecutive features a lane and piece, so the variance is that
+// of the centred values, and four neighbouring lanes hold one block of a checkpoint.  The next row is on its way while this
+// one is worked on, and loads are never behind a branch that waits for them: those of a wide row's last piece start up to
+// seven elements early, where a whole one still fits, and are shifted into place in registers.  Statistics and sums are
+// fp32.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "fa.h"
 #include "fa_layers.h"
@@ -25,10 +29,83 @@ __device__ __forceinline__ float team_sum(float v) {
   return v;
 }
 
+// Eight consecutive elements as they lie in memory.
+template <typename T>
+struct raw8 {
+  fa_u32x4 u[sizeof(T) / 2];
+};
+__device__ __forceinline__ raw8<fa_bf16> load_whole(const fa_bf16* p) {
+  return {{*reinterpret_cast<const fa_u32x4_2*>(p)}};
+}
+__device__ __forceinline__ raw8<float> load_whole(const float* p) {
+  return {{*reinterpret_cast<const fa_u32x4_4*>(p), *reinterpret_cast<const fa_u32x4_4*>(p + 4)}};
+}
+// The eight elements from `at` of a row of D, zeros past its end.  LAST: the piece may be past the end, or end behind it;
+// then the load starts at D - 8, and place() moves it.
+template <bool LAST, typename T>
+__device__ __forceinline__ raw8<T> load_piece(const T* row, int at, int D) {
+  if constexpr (!LAST) return load_whole(row + at);
+  raw8<T> r = {};
+  if (D >= 8) {
+    if (at < D) r = load_whole(row + min(at, D - 8));
+  } else if (at == 0) {
+    float v[8];
+    fa_load8(row, D, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (sizeof(T) == 4) r.u[e >> 2][e & 3] = __float_as_uint(v[e]);
+      else r.u[0][e >> 1] |= (__float_as_uint(v[e]) >> 16) << (16 * (e & 1));
+    }
+  }
+  return r;
+}
+template <typename T, int WORDS>
+__device__ __forceinline__ void shift_words(raw8<T>& r, bool on) {
+  constexpr int N = 4 * (int)(sizeof(T) / 2);
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const uint32_t from = k + WORDS < N ? r.u[(k + WORDS) >> 2][(k + WORDS) & 3] : 0u;
+    r.u[k >> 2][k & 3] = on ? from : r.u[k >> 2][k & 3];
+  }
+}
+__device__ __forceinline__ void place(raw8<float>& r, int by) {
+  shift_words<float, 4>(r, by & 4);
+  shift_words<float, 2>(r, by & 2);
+  shift_words<float, 1>(r, by & 1);
+}
+__device__ __forceinline__ void place(raw8<fa_bf16>& r, int by) {
+  shift_words<fa_bf16, 2>(r, by & 4);
+  shift_words<fa_bf16, 1>(r, by & 2);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t next = k < 3 ? r.u[0][k + 1] : 0u;
+    r.u[0][k] = by & 1 ? __builtin_amdgcn_alignbit(next, r.u[0][k], 16) : r.u[0][k];
+  }
+}
+template <bool LAST, typename T>
+__device__ __forceinline__ void values(raw8<T> r, int at, int D, float v[8]) {
+  if constexpr (LAST) {
+    if ((D & 7) && D >= 8) place(r, at < D ? max(at - (D - 8), 0) : 0);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if constexpr (sizeof(T) == 4) v[e] = __uint_as_float(r.u[e >> 2][e & 3]);
+    else v[e] = __uint_as_float(e & 1 ? r.u[0][e >> 1] & 0xffff0000u : r.u[0][e >> 1] << 16);
+  }
+}
+// calls f(c, last) for the pieces 0..NC - 1, `last` a constant type of its call
+template <int NC, typename F>
+__device__ __forceinline__ void each_piece(F f) {
+  if constexpr (NC > 1) each_piece<NC - 1>([&](auto c, auto) __attribute__((always_inline)) {
+    f(c, std::integral_constant<bool, false>());
+  });
+  f(std::integral_constant<int, NC - 1>(), std::integral_constant<bool, true>());
+}
+
 }  // namespace
 
 // T: storage of x and y; a row's team is L lanes of a wavefront (W = 1) or W whole wavefronts, with NC pieces of eight
-// features a lane.
+// features a lane: 8 L W (NC - 1) < D <= 8 L W NC (or NC = 1).
 template <typename T, int L, int NC, int W>
 __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_kernel(fa_norm_args a) {
   static_assert(W == 1 || L == 64, "a team of several wavefronts uses all their lanes");
@@ -37,17 +114,36 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_kerne
   __shared__ float red[2][W];
   const int lane = threadIdx.x % TL, D = a.features;
   const float width = (float)D;
-  for (int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TL; row < a.rows; row += (int64_t)gridDim.x * TEAMS) {
-    const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+  const int64_t pitch = fa_code_pitch(D), epitch = fa_exponent_pitch(D);
+  const T* x = static_cast<const T*>(a.x);
+  int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TL;
+  const int64_t step = (int64_t)gridDim.x * TEAMS;
+  raw8<T> next[NC];
+  if (row < a.rows)
+    each_piece<NC>([&](auto c, auto last) __attribute__((always_inline)) {
+      next[c] = load_piece<last>(x + row * a.ldx, 8 * (lane + TL * c), D);
+    });
+  float gamma[NC][8], beta[NC][8];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int at = 8 * (lane + TL * c);
+    if (a.gamma) fa_load8_param(a.gamma, a.param_bf16, at, D - at, gamma[c]);
+    if (a.beta) fa_load8_param(a.beta, a.param_bf16, at, D - at, beta[c]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (!a.gamma) gamma[c][e] = 1.f;
+      if (!a.beta) beta[c][e] = 0.f;
+    }
+  }
+  for (; row < a.rows; row += step) {
     float v[NC][8];
     float s = 0.f;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int at = 8 * (lane + TL * c);
-      fa_load8(x + at, D - at, v[c]);
+    each_piece<NC>([&](auto c, auto last) __attribute__((always_inline)) {
+      values<last>(next[c], 8 * (lane + TL * c), D, v[c]);
+      if (row + step < a.rows) next[c] = load_piece<last>(x + (row + step) * a.ldx, 8 * (lane + TL * c), D);
 #pragma unroll
       for (int e = 0; e < 8; ++e) s += v[c][e];
-    }
+    });
     s = team_sum<L>(s);
     if constexpr (W > 1) {
       if (threadIdx.x % 64 == 0) red[0][threadIdx.x / 64] = s;
@@ -58,15 +154,14 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_kerne
     }
     const float mean = s / width;
     float q = 0.f;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int at = 8 * (lane + TL * c);
+    each_piece<NC>([&](auto c, auto last) __attribute__((always_inline)) {
+      const int valid = D - 8 * (lane + TL * c);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        v[c][e] = at + e < D ? v[c][e] - mean : 0.f;
+        v[c][e] = !last || e < valid ? v[c][e] - mean : 0.f;
         q += v[c][e] * v[c][e];
       }
-    }
+    });
     q = team_sum<L>(q);
     if constexpr (W > 1) {
       if (threadIdx.x % 64 == 0) red[1][threadIdx.x / 64] = q;
@@ -81,39 +176,31 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_kerne
       if (a.rstd) a.rstd[row] = rstd;
     }
     T* y = static_cast<T*>(a.y) + row * a.ldy;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
+    each_piece<NC>([&](auto c, auto last) __attribute__((always_inline)) {
       const int at = 8 * (lane + TL * c);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[c][e] = at + e < D ? v[c][e] * rstd : 0.f;
+      for (int e = 0; e < 8; ++e) v[c][e] *= rstd;
       if (a.codes) {
+        // (past the end of a row of an infinite or NaN rstd there is no 0 but NaN: its block has that anyway)
         const uint32_t e = fa_block_exponent(fa_quad_most(v[c]));
-        const int64_t pitch = fa_code_pitch(D);
-        if (at < pitch) {
+        if (!last || at < pitch) {
           *reinterpret_cast<uint2*>(a.codes + row * pitch + at) = fa_codes8(v[c], e);
-          if ((lane & 3) == 0) a.exponents[row * fa_exponent_pitch(D) + (at >> 5)] = (uint8_t)e;
+          if ((lane & 3) == 0) a.exponents[row * epitch + (at >> 5)] = (uint8_t)e;
         }
       }
-      float g[8], b[8];
-      if (a.gamma) {
-        fa_load8_param(a.gamma, a.param_bf16, at, D - at, g);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[c][e] *= g[e];
-      }
-      if (a.beta) {
-        fa_load8_param(a.beta, a.param_bf16, at, D - at, b);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[c][e] += b[e];
-      }
-      fa_store8(y + at, D - at, v[c]);
-    }
+      for (int e = 0; e < 8; ++e) v[c][e] = v[c][e] * gamma[c][e] + beta[c][e];
+      if constexpr (last) fa_store8(y + at, D - at, v[c]);
+      else fa_store8_whole(y + at, v[c]);
+    });
   }
 }
 
 namespace {
 
-// Rows that one workgroup of the backward pass takes: a share of one worker's.  About kNormBlocks workgroups in all.
-constexpr int kNormBlocks = 1024;
+// Rows that one workgroup of the backward pass takes: a share of one worker's.  About kNormBlocks workgroups in all, three
+// for every compute unit, which is what their registers allow.
+constexpr int kNormBlocks = 768;
 
 struct norm_chunks {
   int first[FA_P_MAX + 1];   // worker w has the chunks [first[w], first[w + 1])
@@ -140,7 +227,7 @@ __device__ __forceinline__ int worker_of(const int* first, int p, int k) {
 }  // namespace
 
 // T: storage of dy, x, dx; KEPT: xhat from the checkpoint.  One workgroup takes one chunk of rows of one worker and leaves
-// its share of dgamma and dbeta in partials[chunk][2][D].
+// its share of dgamma and dbeta in partials[chunk][2][D].  Teams and pieces as above.
 template <typename T, bool KEPT, int L, int NC, int W>
 __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_backward_kernel(fa_norm_grad_args a, norm_chunks ch) {
   constexpr int TL = L * W;
@@ -155,48 +242,75 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_backw
   const int w = worker_of(ch.first, a.blocks.p, blockIdx.x);
   const int64_t begin = a.blocks.row0[w] + (int64_t)(blockIdx.x - ch.first[w]) * ch.rows_per_chunk;
   const int64_t end = min(begin + ch.rows_per_chunk, a.blocks.row0[w + 1]);
-  float dg[NC][8], db[NC][8];
-#pragma unroll
-  for (int c = 0; c < NC; ++c)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) dg[c][e] = db[c][e] = 0.f;
-  int turn = 0;
-  for (int64_t row = begin + threadIdx.x / TL; row < end; row += TEAMS, turn ^= 1) {
-    const T* dy = static_cast<const T*>(a.dy) + row * a.lddy;
-    const float rstd = a.rstd[row];
-    float xh[NC][8], h[NC][8];
-    float s = 0.f, q = 0.f;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
+  const T* dy = static_cast<const T*>(a.dy);
+  const T* x = static_cast<const T*>(a.x);
+  const T* residual = static_cast<const T*>(a.residual);
+  raw8<T> next_dy[NC], next_x[KEPT ? 1 : NC], next_res[NC];
+  uint2 next_codes[KEPT ? NC : 1];
+  uint32_t next_e[KEPT ? NC : 1];
+  float next_mean = 0.f, next_rstd = 0.f;
+  auto load = [&](int64_t row) __attribute__((always_inline)) {
+    next_rstd = a.rstd[row];
+    if constexpr (!KEPT) next_mean = a.mean[row];
+    each_piece<NC>([&](auto c, auto last) __attribute__((always_inline)) {
       const int at = 8 * (lane + TL * c);
-      fa_load8(dy + at, D - at, h[c]);
+      next_dy[c] = load_piece<last>(dy + row * a.lddy, at, D);
       if constexpr (KEPT) {
-        if (at < pitch) {
-          const uint2 codes = *reinterpret_cast<const uint2*>(a.codes + row * pitch + at);
-          fa_values8(codes, fa_block_scale(a.exponents[row * epitch + (at >> 5)]), xh[c]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) xh[c][e] = 0.f;
+        next_codes[c] = make_uint2(0u, 0u);
+        next_e[c] = 0u;
+        if (!last || at < pitch) {
+          next_codes[c] = *reinterpret_cast<const uint2*>(a.codes + row * pitch + at);
+          next_e[c] = a.exponents[row * epitch + (at >> 5)];
         }
       } else {
-        fa_load8(static_cast<const T*>(a.x) + row * a.ldx + at, D - at, xh[c]);
-        const float mean = a.mean[row];
+        next_x[c] = load_piece<last>(x + row * a.ldx, at, D);
+      }
+      if (residual) next_res[c] = load_piece<last>(residual + row * a.ldr, at, D);
+    });
+  };
+  int64_t row = begin + threadIdx.x / TL;
+  if (row < end) load(row);
+  float gamma[NC][8], dg[NC][8], db[NC][8];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int at = 8 * (lane + TL * c);
+    if (a.gamma) fa_load8_param(a.gamma, a.param_bf16, at, D - at, gamma[c]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      dg[c][e] = db[c][e] = 0.f;
+      if (!a.gamma) gamma[c][e] = 1.f;
+    }
+  }
+  int turn = 0;
+  for (; row < end; row += TEAMS, turn ^= 1) {
+    const float rstd = next_rstd, mean = next_mean;
+    float xh[NC][8], h[NC][8];
+    raw8<T> res[NC];
+    // (what lies past the end of the row is zero in h, and so adds nothing)
+    each_piece<NC>([&](auto c, auto last) __attribute__((always_inline)) {
+      const int at = 8 * (lane + TL * c);
+      values<last>(next_dy[c], at, D, h[c]);
+      if constexpr (KEPT) {
+        fa_values8(next_codes[c], fa_block_scale(next_e[c]), xh[c]);
+      } else {
+        values<last>(next_x[c], at, D, xh[c]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) xh[c][e] = (xh[c][e] - mean) * rstd;
       }
-      float g[8];
-      if (a.gamma) fa_load8_param(a.gamma, a.param_bf16, at, D - at, g);
+      if (residual) res[c] = next_res[c];
+    });
+    if (row + TEAMS < end) load(row + TEAMS);
+    float s = 0.f, q = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if (at + e < D) {
-          db[c][e] += h[c][e];
-          dg[c][e] += h[c][e] * xh[c][e];
-          if (a.gamma) h[c][e] *= g[e];
-          s += h[c][e];
-          q += h[c][e] * xh[c][e];
-        }
+        db[c][e] += h[c][e];
+        dg[c][e] += h[c][e] * xh[c][e];
+        h[c][e] *= gamma[c][e];
+        s += h[c][e];
+        q += h[c][e] * xh[c][e];
       }
-    }
     s = team_sum<L>(s);
     q = team_sum<L>(q);
     if constexpr (W > 1) {
@@ -213,19 +327,19 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_backw
     s /= width;
     q /= width;
     T* dx = static_cast<T*>(a.dx) + row * a.lddx;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
+    each_piece<NC>([&](auto c, auto last) __attribute__((always_inline)) {
       const int at = 8 * (lane + TL * c);
 #pragma unroll
       for (int e = 0; e < 8; ++e) h[c][e] = rstd * (h[c][e] - s - xh[c][e] * q);
-      if (a.residual) {
+      if (residual) {
         float r[8];
-        fa_load8(static_cast<const T*>(a.residual) + row * a.ldr + at, D - at, r);
+        values<last>(res[c], at, D, r);
 #pragma unroll
         for (int e = 0; e < 8; ++e) h[c][e] += r[e];
       }
-      fa_store8(dx + at, D - at, h[c]);
-    }
+      if constexpr (last) fa_store8(dx + at, D - at, h[c]);
+      else fa_store8_whole(dx + at, h[c]);
+    });
   }
   if (!a.dgamma && !a.dbeta) return;
   float* part = a.partials + (int64_t)blockIdx.x * 2 * D;
@@ -269,20 +383,32 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_backw
   }
 }
 
-// dgamma (blockIdx.z = 0) and dbeta (1) of one worker: its chunks' shares, four interleaved sums joined in their order.
+// dgamma (blockIdx.z = 0) and dbeta (1) of one worker: its chunks' shares in eight interleaved sums, these in their order.
 __global__ __launch_bounds__(kThreads) void fa_layer_norm_grads_kernel(fa_norm_grad_args a, norm_chunks ch) {
-  __shared__ float red[4][64];
+  constexpr int GROUPS = 8, COLUMNS = kThreads / GROUPS, DEEP = 8;
+  __shared__ float red[GROUPS][COLUMNS];
   const int w = blockIdx.y, which = blockIdx.z, D = a.features;
   void* out = which ? a.dbeta : a.dgamma;
   if (!out) return;
-  const int j = blockIdx.x * 64 + threadIdx.x % 64, group = threadIdx.x / 64;
+  const int j = blockIdx.x * COLUMNS + threadIdx.x % COLUMNS, group = threadIdx.x / COLUMNS;
   float s = 0.f;
   if (j < D)
-    for (int k = ch.first[w] + group; k < ch.first[w + 1]; k += 4) s += a.partials[((int64_t)k * 2 + which) * D + j];
-  red[group][threadIdx.x % 64] = s;
+    for (int k = ch.first[w] + group; k < ch.first[w + 1]; k += GROUPS * DEEP) {
+      float v[DEEP];
+#pragma unroll
+      for (int n = 0; n < DEEP; ++n) {
+        const int at = k + GROUPS * n;
+        v[n] = at < ch.first[w + 1] ? a.partials[((int64_t)at * 2 + which) * D + j] : 0.f;
+      }
+#pragma unroll
+      for (int n = 0; n < DEEP; ++n) s += v[n];
+    }
+  red[group][threadIdx.x % COLUMNS] = s;
   __syncthreads();
   if (group == 0 && j < D) {
-    s = red[0][threadIdx.x] + red[1][threadIdx.x] + red[2][threadIdx.x] + red[3][threadIdx.x];
+    s = 0.f;
+#pragma unroll
+    for (int n = 0; n < GROUPS; ++n) s += red[n][threadIdx.x];
     const int64_t at = (int64_t)w * (which ? a.lddbeta : a.lddgamma) + j;
     if (a.grad_bf16) fa_store1(static_cast<fa_bf16*>(out) + at, s);
     else fa_store1(static_cast<float*>(out) + at, s);
@@ -331,25 +457,31 @@ int grid_for(int64_t threads) {
 }
 
 template <typename T, int L, int NC, int W>
-hipError_t norm(const fa_norm_args& a, hipStream_t st) {
+void norm(const fa_norm_args& a, hipStream_t st) {
   const int teams = W > 1 ? 1 : kThreads / L;
   int64_t blocks = (a.rows + teams - 1) / teams;
-  if (blocks > 4096) blocks = 4096;
+  if (blocks > 2048) blocks = 2048;
   hipLaunchKernelGGL((fa_layer_norm_kernel<T, L, NC, W>), dim3((unsigned)blocks), dim3(W > 1 ? 64 * W : kThreads), 0, st, a);
-  return hipGetLastError();
 }
 
+// The team of a width: no more lanes than the row has work for, all pieces but the last whole.
 template <typename T>
 hipError_t norm_of(const fa_norm_args& a, hipStream_t st) {
   const int D = a.features;
-  if (D <= 32) return norm<T, 4, 1, 1>(a, st);
-  if (D <= 128) return norm<T, 16, 1, 1>(a, st);
-  if (D <= 512) return norm<T, 64, 1, 1>(a, st);
-  if (D <= 1024) return norm<T, 64, 2, 1>(a, st);
-  if (D <= 2048) return norm<T, 64, 4, 1>(a, st);
-  if (D <= 4096) return norm<T, 64, 2, 4>(a, st);
-  if (D <= 8192) return norm<T, 64, 4, 4>(a, st);
-  return norm<T, 64, 8, 4>(a, st);
+  if (D <= 32) norm<T, 4, 1, 1>(a, st);
+  else if (D <= 128) norm<T, 16, 1, 1>(a, st);
+  else if (D <= 256) norm<T, 16, 2, 1>(a, st);
+  else if (D <= 512) norm<T, 32, 2, 1>(a, st);
+  else if (D <= 768) norm<T, 32, 3, 1>(a, st);
+  else if (D <= 1024) norm<T, 64, 2, 1>(a, st);
+  else if (D <= 1536) norm<T, 64, 3, 1>(a, st);
+  else if (D <= 2048) norm<T, 64, 4, 1>(a, st);
+  else if (D <= 4096) norm<T, 64, 2, 4>(a, st);
+  else if (D <= 6144) norm<T, 64, 3, 4>(a, st);
+  else if (D <= 8192) norm<T, 64, 4, 4>(a, st);
+  else if (D <= 12288) norm<T, 64, 3, 8>(a, st);
+  else norm<T, 64, 4, 8>(a, st);
+  return hipGetLastError();
 }
 
 template <typename T, bool KEPT, int L, int NC, int W>
@@ -363,11 +495,15 @@ void norm_backward_of(const fa_norm_grad_args& a, const norm_chunks& ch, hipStre
   const int D = a.features;
   if (D <= 32) norm_backward<T, KEPT, 4, 1, 1>(a, ch, st);
   else if (D <= 128) norm_backward<T, KEPT, 16, 1, 1>(a, ch, st);
-  else if (D <= 512) norm_backward<T, KEPT, 64, 1, 1>(a, ch, st);
+  else if (D <= 256) norm_backward<T, KEPT, 16, 2, 1>(a, ch, st);
+  else if (D <= 512) norm_backward<T, KEPT, 32, 2, 1>(a, ch, st);
+  else if (D <= 768) norm_backward<T, KEPT, 32, 3, 1>(a, ch, st);
   else if (D <= 1024) norm_backward<T, KEPT, 64, 2, 1>(a, ch, st);
   else if (D <= 2048) norm_backward<T, KEPT, 64, 1, 4>(a, ch, st);
   else if (D <= 4096) norm_backward<T, KEPT, 64, 2, 4>(a, ch, st);
+  else if (D <= 6144) norm_backward<T, KEPT, 64, 3, 4>(a, ch, st);
   else if (D <= 8192) norm_backward<T, KEPT, 64, 4, 4>(a, ch, st);
+  else if (D <= 12288) norm_backward<T, KEPT, 64, 3, 8>(a, ch, st);
   else norm_backward<T, KEPT, 64, 4, 8>(a, ch, st);
 }
 
@@ -420,7 +556,7 @@ hipError_t fa_launch_layer_norm_backward(const fa_norm_grad_args& a, int dtype, 
     if (e != hipSuccess) return e;
   }
   if (a.dgamma || a.dbeta)
-    hipLaunchKernelGGL(fa_layer_norm_grads_kernel, dim3((unsigned)((a.features + 63) / 64), (unsigned)a.blocks.p, 2),
+    hipLaunchKernelGGL(fa_layer_norm_grads_kernel, dim3((unsigned)((a.features + 31) / 32), (unsigned)a.blocks.p, 2),
                        dim3(kThreads), 0, st, a, ch);
   return hipGetLastError();
 }
