@@ -7,9 +7,7 @@
 // Bound by memory: forward reads x and writes y and the checkpoint, backward reads dy and xhat and writes dx, every element
 // once.  A row is held in registers by a team of lanes, eight consecutive features a lane and piece, so the variance is that
 // of the centred values, and four neighbouring lanes hold one block of a checkpoint.  The next row is on its way while this
-// one is worked on, and loads are never behind a branch that waits for them: those of a wide row's last piece start up to
-// seven elements early, where a whole one still fits, and are shifted into place in registers.  Statistics and sums are
-// fp32.
+// one is worked on.  Statistics and sums are fp32.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <type_traits>
@@ -29,6 +27,8 @@ __device__ __forceinline__ float team_sum(float v) {
   return v;
 }
 
+typedef unsigned int vec_u32x4 __attribute__((__vector_size__(16)));
+
 // Eight consecutive elements as they lie in memory.
 template <typename T>
 struct raw8 {
@@ -40,57 +40,92 @@ __device__ __forceinline__ raw8<fa_bf16> load_whole(const fa_bf16* p) {
 __device__ __forceinline__ raw8<float> load_whole(const float* p) {
   return {{*reinterpret_cast<const fa_u32x4_4*>(p), *reinterpret_cast<const fa_u32x4_4*>(p + 4)}};
 }
-// The eight elements from `at` of a row of D, zeros past its end.  LAST: the piece may be past the end, or end behind it;
-// then the load starts at D - 8, and place() moves it.
-template <bool LAST, typename T>
-__device__ __forceinline__ raw8<T> load_piece(const T* row, int at, int D) {
-  if constexpr (!LAST) return load_whole(row + at);
-  raw8<T> r = {};
-  if (D >= 8) {
-    if (at < D) r = load_whole(row + min(at, D - 8));
-  } else if (at == 0) {
+// One row of D elements, read and written in pieces of eight from `at`; what is past its end reads as zero and is not
+// written.  A row of a whole wavefront or more (WIDE: its address is the same for every lane) is a buffer, and the memory
+// unit looks after its end, in steps of four bytes: no branch stands between a load and the next.  The last element of an
+// odd row of bf16 comes alone.
+template <bool WIDE, typename T>
+struct row_in;
+template <typename T>
+struct row_in<true, T> {
+  __amdgpu_buffer_rsrc_t r;
+  const T* end;
+  __device__ __forceinline__ row_in(const T* p, int D)
+      : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(p), 0, D * (int)sizeof(T) & ~3, 0x00020000)), end(p + D - 1) {}
+  __device__ __forceinline__ raw8<T> load(int at, int) const {
+    raw8<T> v;
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k)
+      v.u[k] = __builtin_bit_cast(fa_u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at * (int)sizeof(T) + 16 * k, 0, 0));
+    return v;
+  }
+  __device__ __forceinline__ uint32_t last() const { return sizeof(T) == 2 ? (uint32_t)*reinterpret_cast<const uint16_t*>(end) : 0u; }
+};
+// A row of fewer lanes: the piece that the row ends in is loaded element by element.
+template <typename T>
+struct row_in<false, T> {
+  const T* p;
+  __device__ __forceinline__ row_in(const T* row, int) : p(row) {}
+  __device__ __forceinline__ raw8<T> load(int at, int D) const {
+    if (at + 8 <= D) return load_whole(p + at);
+    raw8<T> r = {};
     float v[8];
-    fa_load8(row, D, v);
+    fa_load8(p + at, D - at, v);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       if constexpr (sizeof(T) == 4) r.u[e >> 2][e & 3] = __float_as_uint(v[e]);
       else r.u[0][e >> 1] |= (__float_as_uint(v[e]) >> 16) << (16 * (e & 1));
     }
+    return r;
   }
-  return r;
-}
-template <typename T, int WORDS>
-__device__ __forceinline__ void shift_words(raw8<T>& r, bool on) {
-  constexpr int N = 4 * (int)(sizeof(T) / 2);
-#pragma unroll
-  for (int k = 0; k < N; ++k) {
-    const uint32_t from = k + WORDS < N ? r.u[(k + WORDS) >> 2][(k + WORDS) & 3] : 0u;
-    r.u[k >> 2][k & 3] = on ? from : r.u[k >> 2][k & 3];
-  }
-}
-__device__ __forceinline__ void place(raw8<float>& r, int by) {
-  shift_words<float, 4>(r, by & 4);
-  shift_words<float, 2>(r, by & 2);
-  shift_words<float, 1>(r, by & 1);
-}
-__device__ __forceinline__ void place(raw8<fa_bf16>& r, int by) {
-  shift_words<fa_bf16, 2>(r, by & 4);
-  shift_words<fa_bf16, 1>(r, by & 2);
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const uint32_t next = k < 3 ? r.u[0][k + 1] : 0u;
-    r.u[0][k] = by & 1 ? __builtin_amdgcn_alignbit(next, r.u[0][k], 16) : r.u[0][k];
-  }
-}
-template <bool LAST, typename T>
-__device__ __forceinline__ void values(raw8<T> r, int at, int D, float v[8]) {
-  if constexpr (LAST) {
-    if ((D & 7) && D >= 8) place(r, at < D ? max(at - (D - 8), 0) : 0);
-  }
+  __device__ __forceinline__ uint32_t last() const { return 0u; }
+};
+// as floats; `last` belongs into the row's last piece
+template <bool WIDE, bool LAST, typename T>
+__device__ __forceinline__ void values(raw8<T> r, uint32_t last, int at, int D, float v[8]) {
+  // (held back to here: the compiler would convert a row where it arrives, and wait for it there)
+  asm("" : "+v"(r.u[0]));
+  if constexpr (sizeof(T) == 4) asm("" : "+v"(r.u[1]));
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     if constexpr (sizeof(T) == 4) v[e] = __uint_as_float(r.u[e >> 2][e & 3]);
     else v[e] = __uint_as_float(e & 1 ? r.u[0][e >> 1] & 0xffff0000u : r.u[0][e >> 1] << 16);
+  }
+  if constexpr (WIDE && LAST && sizeof(T) == 2) {
+    if (D & 1) {
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) v[e] = at + e == D - 1 ? __uint_as_float(last << 16) : v[e];
+    }
+  }
+}
+template <bool WIDE, bool LAST, typename T>
+__device__ __forceinline__ void store_piece(T* row, int at, int D, const float v[8]) {
+  if constexpr (!LAST) {
+    fa_store8_whole(row + at, v);
+  } else if constexpr (!WIDE) {
+    fa_store8(row + at, D - at, v);
+  } else {
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(row, 0, D * (int)sizeof(T) & ~3, 0x00020000);
+    fa_u32x4 u[2];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (sizeof(T) == 4) {
+        u[0][k] = __float_as_uint(v[k]);
+        u[1][k] = __float_as_uint(v[4 + k]);
+      } else {
+        u[0][k] = fa_pack_bf16(v[2 * k], v[2 * k + 1]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k)
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(vec_u32x4, u[k]), r, at * (int)sizeof(T) + 16 * k, 0, 0);
+    if constexpr (sizeof(T) == 2) {
+      if (D & 1) {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2)
+          if (at + e == D - 1) fa_store1(row + D - 1, v[e]);
+      }
+    }
   }
 }
 // calls f(c, last) for the pieces 0..NC - 1, `last` a constant type of its call
@@ -115,14 +150,22 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_kerne
   const int lane = threadIdx.x % TL, D = a.features;
   const float width = (float)D;
   const int64_t pitch = fa_code_pitch(D), epitch = fa_exponent_pitch(D);
+  constexpr bool WIDE = L == 64;
   const T* x = static_cast<const T*>(a.x);
-  int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TL;
+  int team = threadIdx.x / TL;
+  if constexpr (WIDE) team = __builtin_amdgcn_readfirstlane(team);
+  int64_t row = (int64_t)blockIdx.x * TEAMS + team;
   const int64_t step = (int64_t)gridDim.x * TEAMS;
+  if (W == 1 && row >= a.rows) return;
   raw8<T> next[NC];
-  if (row < a.rows)
-    each_piece<NC>([&](auto c, auto last) __attribute__((always_inline)) {
-      next[c] = load_piece<last>(x + row * a.ldx, 8 * (lane + TL * c), D);
-    });
+  uint32_t next_last = 0;
+  auto load = [&](int64_t r) __attribute__((always_inline)) {
+    const row_in<WIDE, T> in(x + r * a.ldx, D);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) next[c] = in.load(8 * (lane + TL * c), D);
+    next_last = in.last();
+  };
+  load(row);
   float gamma[NC][8], beta[NC][8];
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
@@ -139,11 +182,11 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_kerne
     float v[NC][8];
     float s = 0.f;
     each_piece<NC>([&](auto c, auto last) __attribute__((always_inline)) {
-      values<last>(next[c], 8 * (lane + TL * c), D, v[c]);
-      if (row + step < a.rows) next[c] = load_piece<last>(x + (row + step) * a.ldx, 8 * (lane + TL * c), D);
+      values<WIDE, last>(next[c], next_last, 8 * (lane + TL * c), D, v[c]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) s += v[c][e];
     });
+    load(row + step < a.rows ? row + step : row);       // (the last row comes again: a load that nothing waits for)
     s = team_sum<L>(s);
     if constexpr (W > 1) {
       if (threadIdx.x % 64 == 0) red[0][threadIdx.x / 64] = s;
@@ -190,8 +233,7 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_kerne
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[c][e] = v[c][e] * gamma[c][e] + beta[c][e];
-      if constexpr (last) fa_store8(y + at, D - at, v[c]);
-      else fa_store8_whole(y + at, v[c]);
+      store_piece<WIDE, last>(y, at, D, v[c]);
     });
   }
 }
@@ -242,33 +284,58 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_backw
   const int w = worker_of(ch.first, a.blocks.p, blockIdx.x);
   const int64_t begin = a.blocks.row0[w] + (int64_t)(blockIdx.x - ch.first[w]) * ch.rows_per_chunk;
   const int64_t end = min(begin + ch.rows_per_chunk, a.blocks.row0[w + 1]);
+  constexpr bool WIDE = L == 64;
   const T* dy = static_cast<const T*>(a.dy);
   const T* x = static_cast<const T*>(a.x);
   const T* residual = static_cast<const T*>(a.residual);
   raw8<T> next_dy[NC], next_x[KEPT ? 1 : NC], next_res[NC];
   uint2 next_codes[KEPT ? NC : 1];
   uint32_t next_e[KEPT ? NC : 1];
+  uint32_t last_dy = 0, last_x = 0, last_res = 0;
   float next_mean = 0.f, next_rstd = 0.f;
   auto load = [&](int64_t row) __attribute__((always_inline)) {
     next_rstd = a.rstd[row];
-    if constexpr (!KEPT) next_mean = a.mean[row];
-    each_piece<NC>([&](auto c, auto last) __attribute__((always_inline)) {
-      const int at = 8 * (lane + TL * c);
-      next_dy[c] = load_piece<last>(dy + row * a.lddy, at, D);
-      if constexpr (KEPT) {
-        next_codes[c] = make_uint2(0u, 0u);
-        next_e[c] = 0u;
-        if (!last || at < pitch) {
-          next_codes[c] = *reinterpret_cast<const uint2*>(a.codes + row * pitch + at);
-          next_e[c] = a.exponents[row * epitch + (at >> 5)];
+    const row_in<WIDE, T> in(dy + row * a.lddy, D);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) next_dy[c] = in.load(8 * (lane + TL * c), D);
+    last_dy = in.last();
+    if constexpr (KEPT) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int at = 8 * (lane + TL * c);
+        if constexpr (WIDE) {
+          const __amdgpu_buffer_rsrc_t codes =
+              __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(a.codes) + row * pitch, 0, (int)pitch, 0x00020000);
+          const __amdgpu_buffer_rsrc_t exponents =
+              __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.exponents) + row * epitch, 0, (int)pitch / 32, 0x00020000);
+          next_codes[c] = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(codes, at, 0, 0));
+          next_e[c] = __builtin_amdgcn_raw_buffer_load_b8(exponents, at >> 5, 0, 0);
+        } else {
+          next_codes[c] = make_uint2(0u, 0u);
+          next_e[c] = 0u;
+          if (at < pitch) {
+            next_codes[c] = *reinterpret_cast<const uint2*>(a.codes + row * pitch + at);
+            next_e[c] = a.exponents[row * epitch + (at >> 5)];
+          }
         }
-      } else {
-        next_x[c] = load_piece<last>(x + row * a.ldx, at, D);
       }
-      if (residual) next_res[c] = load_piece<last>(residual + row * a.ldr, at, D);
-    });
+    } else {
+      next_mean = a.mean[row];
+      const row_in<WIDE, T> from(x + row * a.ldx, D);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) next_x[c] = from.load(8 * (lane + TL * c), D);
+      last_x = from.last();
+    }
+    if (residual) {
+      const row_in<WIDE, T> more(residual + row * a.ldr, D);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) next_res[c] = more.load(8 * (lane + TL * c), D);
+      last_res = more.last();
+    }
   };
-  int64_t row = begin + threadIdx.x / TL;
+  int team = threadIdx.x / TL;
+  if constexpr (WIDE) team = __builtin_amdgcn_readfirstlane(team);
+  int64_t row = begin + team;
   if (row < end) load(row);
   float gamma[NC][8], dg[NC][8], db[NC][8];
 #pragma unroll
@@ -287,19 +354,21 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_backw
     float xh[NC][8], h[NC][8];
     raw8<T> res[NC];
     // (what lies past the end of the row is zero in h, and so adds nothing)
+    const uint32_t end_res = last_res;
     each_piece<NC>([&](auto c, auto last) __attribute__((always_inline)) {
       const int at = 8 * (lane + TL * c);
-      values<last>(next_dy[c], at, D, h[c]);
+      values<WIDE, last>(next_dy[c], last_dy, at, D, h[c]);
       if constexpr (KEPT) {
+        asm("" : "+v"(next_codes[c].x), "+v"(next_codes[c].y), "+v"(next_e[c]));
         fa_values8(next_codes[c], fa_block_scale(next_e[c]), xh[c]);
       } else {
-        values<last>(next_x[c], at, D, xh[c]);
+        values<WIDE, last>(next_x[c], last_x, at, D, xh[c]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) xh[c][e] = (xh[c][e] - mean) * rstd;
       }
       if (residual) res[c] = next_res[c];
     });
-    if (row + TEAMS < end) load(row + TEAMS);
+    load(row + TEAMS < end ? row + TEAMS : row);
     float s = 0.f, q = 0.f;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
@@ -333,12 +402,11 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_backw
       for (int e = 0; e < 8; ++e) h[c][e] = rstd * (h[c][e] - s - xh[c][e] * q);
       if (residual) {
         float r[8];
-        values<last>(res[c], at, D, r);
+        values<WIDE, last>(res[c], end_res, at, D, r);
 #pragma unroll
         for (int e = 0; e < 8; ++e) h[c][e] += r[e];
       }
-      if constexpr (last) fa_store8(dx + at, D - at, h[c]);
-      else fa_store8_whole(dx + at, h[c]);
+      store_piece<WIDE, last>(dx, at, D, h[c]);
     });
   }
   if (!a.dgamma && !a.dbeta) return;
@@ -456,8 +524,16 @@ int grid_for(int64_t threads) {
   return (int)(blocks < 1 ? 1 : blocks > 8192 ? 8192 : blocks);
 }
 
-template <typename T, int L, int NC, int W>
+// A team for the widths LOW < D <= HIGH: all its pieces but the last are whole, which the kernels take for granted.
+template <int LOW, int HIGH, int L_, int NC_, int W_>
+struct team_of {
+  static constexpr int L = L_, NC = NC_, W = W_;
+  static_assert(HIGH <= 8 * L * W * NC && LOW >= 8 * L * W * (NC - 1), "the pieces of a row");
+};
+
+template <typename T, typename TEAM>
 void norm(const fa_norm_args& a, hipStream_t st) {
+  constexpr int L = TEAM::L, NC = TEAM::NC, W = TEAM::W;
   const int teams = W > 1 ? 1 : kThreads / L;
   int64_t blocks = (a.rows + teams - 1) / teams;
   if (blocks > 2048) blocks = 2048;
@@ -468,24 +544,24 @@ void norm(const fa_norm_args& a, hipStream_t st) {
 template <typename T>
 hipError_t norm_of(const fa_norm_args& a, hipStream_t st) {
   const int D = a.features;
-  if (D <= 32) norm<T, 4, 1, 1>(a, st);
-  else if (D <= 128) norm<T, 16, 1, 1>(a, st);
-  else if (D <= 256) norm<T, 16, 2, 1>(a, st);
-  else if (D <= 512) norm<T, 32, 2, 1>(a, st);
-  else if (D <= 768) norm<T, 32, 3, 1>(a, st);
-  else if (D <= 1024) norm<T, 64, 2, 1>(a, st);
-  else if (D <= 1536) norm<T, 64, 3, 1>(a, st);
-  else if (D <= 2048) norm<T, 64, 4, 1>(a, st);
-  else if (D <= 4096) norm<T, 64, 2, 4>(a, st);
-  else if (D <= 6144) norm<T, 64, 3, 4>(a, st);
-  else if (D <= 8192) norm<T, 64, 4, 4>(a, st);
-  else if (D <= 12288) norm<T, 64, 3, 8>(a, st);
-  else norm<T, 64, 4, 8>(a, st);
+  if (D <= 32) norm<T, team_of<0, 32, 4, 1, 1>>(a, st);
+  else if (D <= 128) norm<T, team_of<32, 128, 16, 1, 1>>(a, st);
+  else if (D <= 256) norm<T, team_of<128, 256, 32, 1, 1>>(a, st);
+  else if (D <= 512) norm<T, team_of<256, 512, 64, 1, 1>>(a, st);
+  else if (D <= 1024) norm<T, team_of<512, 1024, 64, 2, 1>>(a, st);
+  else if (D <= 1536) norm<T, team_of<1024, 1536, 64, 3, 1>>(a, st);
+  else if (D <= 2048) norm<T, team_of<1536, 2048, 64, 4, 1>>(a, st);
+  else if (D <= 4096) norm<T, team_of<2048, 4096, 64, 2, 4>>(a, st);
+  else if (D <= 6144) norm<T, team_of<4096, 6144, 64, 3, 4>>(a, st);
+  else if (D <= 8192) norm<T, team_of<6144, 8192, 64, 4, 4>>(a, st);
+  else if (D <= 12288) norm<T, team_of<8192, 12288, 64, 3, 8>>(a, st);
+  else norm<T, team_of<12288, FA_NORM_FEATURES_MAX, 64, 4, 8>>(a, st);
   return hipGetLastError();
 }
 
-template <typename T, bool KEPT, int L, int NC, int W>
+template <typename T, bool KEPT, typename TEAM>
 void norm_backward(const fa_norm_grad_args& a, const norm_chunks& ch, hipStream_t st) {
+  constexpr int L = TEAM::L, NC = TEAM::NC, W = TEAM::W;
   hipLaunchKernelGGL((fa_layer_norm_backward_kernel<T, KEPT, L, NC, W>), dim3((unsigned)ch.first[FA_P_MAX]),
                      dim3(W > 1 ? 64 * W : kThreads), 0, st, a, ch);
 }
@@ -493,18 +569,16 @@ void norm_backward(const fa_norm_grad_args& a, const norm_chunks& ch, hipStream_
 template <typename T, bool KEPT>
 void norm_backward_of(const fa_norm_grad_args& a, const norm_chunks& ch, hipStream_t st) {
   const int D = a.features;
-  if (D <= 32) norm_backward<T, KEPT, 4, 1, 1>(a, ch, st);
-  else if (D <= 128) norm_backward<T, KEPT, 16, 1, 1>(a, ch, st);
-  else if (D <= 256) norm_backward<T, KEPT, 16, 2, 1>(a, ch, st);
-  else if (D <= 512) norm_backward<T, KEPT, 32, 2, 1>(a, ch, st);
-  else if (D <= 768) norm_backward<T, KEPT, 32, 3, 1>(a, ch, st);
-  else if (D <= 1024) norm_backward<T, KEPT, 64, 2, 1>(a, ch, st);
-  else if (D <= 2048) norm_backward<T, KEPT, 64, 1, 4>(a, ch, st);
-  else if (D <= 4096) norm_backward<T, KEPT, 64, 2, 4>(a, ch, st);
-  else if (D <= 6144) norm_backward<T, KEPT, 64, 3, 4>(a, ch, st);
-  else if (D <= 8192) norm_backward<T, KEPT, 64, 4, 4>(a, ch, st);
-  else if (D <= 12288) norm_backward<T, KEPT, 64, 3, 8>(a, ch, st);
-  else norm_backward<T, KEPT, 64, 4, 8>(a, ch, st);
+  if (D <= 32) norm_backward<T, KEPT, team_of<0, 32, 4, 1, 1>>(a, ch, st);
+  else if (D <= 128) norm_backward<T, KEPT, team_of<32, 128, 16, 1, 1>>(a, ch, st);
+  else if (D <= 256) norm_backward<T, KEPT, team_of<128, 256, 32, 1, 1>>(a, ch, st);
+  else if (D <= 512) norm_backward<T, KEPT, team_of<256, 512, 64, 1, 1>>(a, ch, st);
+  else if (D <= 1024) norm_backward<T, KEPT, team_of<512, 1024, 64, 2, 1>>(a, ch, st);
+  else if (D <= 2048) norm_backward<T, KEPT, team_of<1024, 2048, 64, 1, 4>>(a, ch, st);
+  else if (D <= 4096) norm_backward<T, KEPT, team_of<2048, 4096, 64, 2, 4>>(a, ch, st);
+  else if (D <= 8192) norm_backward<T, KEPT, team_of<4096, 8192, 64, 2, 8>>(a, ch, st);
+  else if (D <= 12288) norm_backward<T, KEPT, team_of<8192, 12288, 64, 3, 8>>(a, ch, st);
+  else norm_backward<T, KEPT, team_of<12288, FA_NORM_FEATURES_MAX, 64, 4, 8>>(a, ch, st);
 }
 
 }  // namespace
