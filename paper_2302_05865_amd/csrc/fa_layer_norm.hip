@@ -28,6 +28,7 @@ __device__ __forceinline__ float team_sum(float v) {
 }
 
 typedef unsigned int vec_u32x4 __attribute__((__vector_size__(16)));
+typedef unsigned int vec_u32x2 __attribute__((__vector_size__(8)));
 
 // Eight consecutive elements as they lie in memory.
 template <typename T>
@@ -43,15 +44,19 @@ __device__ __forceinline__ raw8<float> load_whole(const float* p) {
 // One row of D elements, read and written in pieces of eight from `at`; what is past its end reads as zero and is not
 // written.  A row of a whole wavefront or more (WIDE: its address is the same for every lane) is a buffer, and the memory
 // unit looks after its end, in steps of four bytes: no branch stands between a load and the next.  The last element of an
-// odd row of bf16 comes alone.
+// odd row of bf16 comes alone, in the upper half of a word.  (The waits between two rows count the loads and stores that
+// may still be on their way: those are the same for every row, and none of them is in a branch.)
 template <bool WIDE, typename T>
 struct row_in;
 template <typename T>
 struct row_in<true, T> {
-  __amdgpu_buffer_rsrc_t r;
-  const T* end;
+  __amdgpu_buffer_rsrc_t r, whole;
+  int at_last;
+  // (no row, p null: zeros)
   __device__ __forceinline__ row_in(const T* p, int D)
-      : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(p), 0, D * (int)sizeof(T) & ~3, 0x00020000)), end(p + D - 1) {}
+      : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(p), 0, p ? D * (int)sizeof(T) & ~3 : 0, 0x00020000)),
+        whole(__builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(p), 0, p ? D * (int)sizeof(T) : 0, 0x00020000)),
+        at_last(D * (int)sizeof(T) - 4) {}
   __device__ __forceinline__ raw8<T> load(int at, int) const {
     raw8<T> v;
 #pragma unroll
@@ -59,7 +64,9 @@ struct row_in<true, T> {
       v.u[k] = __builtin_bit_cast(fa_u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at * (int)sizeof(T) + 16 * k, 0, 0));
     return v;
   }
-  __device__ __forceinline__ uint32_t last() const { return sizeof(T) == 2 ? (uint32_t)*reinterpret_cast<const uint16_t*>(end) : 0u; }
+  __device__ __forceinline__ uint32_t last() const {
+    return sizeof(T) == 2 ? __builtin_amdgcn_raw_buffer_load_b32(whole, at_last, 0, 0) : 0u;
+  }
 };
 // A row of fewer lanes: the piece that the row ends in is loaded element by element.
 template <typename T>
@@ -94,8 +101,31 @@ __device__ __forceinline__ void values(raw8<T> r, uint32_t last, int at, int D, 
   if constexpr (WIDE && LAST && sizeof(T) == 2) {
     if (D & 1) {
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) v[e] = at + e == D - 1 ? __uint_as_float(last << 16) : v[e];
+      for (int e = 0; e < 8; e += 2) v[e] = at + e == D - 1 ? __uint_as_float(last & 0xffff0000u) : v[e];
     }
+  }
+}
+// *p = v by the one lane that is `here`; p may be null
+template <bool WIDE>
+__device__ __forceinline__ void store_float(float* p, int64_t at, bool here, float v) {
+  if constexpr (WIDE) {
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(p + at, 0, p ? 4 : 0, 0x00020000);
+    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), r, here ? 0 : 4, 0, 0);
+  } else if (here && p) {
+    p[at] = v;
+  }
+}
+// the codes and exponents of a piece of a row (LAST: it may be past the end), the exponent by every fourth lane
+template <bool WIDE, bool LAST>
+__device__ __forceinline__ void store_codes(int8_t* codes, uint8_t* exponents, int64_t pitch, int at, uint2 u, uint32_t e) {
+  if constexpr (WIDE) {
+    const __amdgpu_buffer_rsrc_t c = __builtin_amdgcn_make_buffer_rsrc(codes, 0, (int)pitch, 0x00020000);
+    const __amdgpu_buffer_rsrc_t x = __builtin_amdgcn_make_buffer_rsrc(exponents, 0, (int)pitch / 32, 0x00020000);
+    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(vec_u32x2, u), c, at, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b8((uint8_t)e, x, (at & 31) == 0 ? at >> 5 : (int)pitch, 0, 0);
+  } else if (!LAST || at < pitch) {
+    *reinterpret_cast<uint2*>(codes + at) = u;
+    if ((at & 31) == 0) exponents[at >> 5] = (uint8_t)e;
   }
 }
 template <bool WIDE, bool LAST, typename T>
@@ -139,9 +169,9 @@ __device__ __forceinline__ void each_piece(F f) {
 
 }  // namespace
 
-// T: storage of x and y; a row's team is L lanes of a wavefront (W = 1) or W whole wavefronts, with NC pieces of eight
+// T: storage of x and y; KEEP: with a checkpoint.  A row's team is L lanes of a wavefront (W = 1) or W whole wavefronts, with NC pieces of eight
 // features a lane: 8 L W (NC - 1) < D <= 8 L W NC (or NC = 1).
-template <typename T, int L, int NC, int W>
+template <typename T, bool KEEP, int L, int NC, int W>
 __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_kernel(fa_norm_args a) {
   static_assert(W == 1 || L == 64, "a team of several wavefronts uses all their lanes");
   constexpr int TL = L * W;                                    // lanes of a team
@@ -187,6 +217,7 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_kerne
       for (int e = 0; e < 8; ++e) s += v[c][e];
     });
     load(row + step < a.rows ? row + step : row);       // (the last row comes again: a load that nothing waits for)
+    __builtin_amdgcn_sched_barrier(0);
     s = team_sum<L>(s);
     if constexpr (W > 1) {
       if (threadIdx.x % 64 == 0) red[0][threadIdx.x / 64] = s;
@@ -214,22 +245,17 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_kerne
       for (int w = 0; w < W; ++w) q += red[1][w];
     }
     const float rstd = 1.f / sqrtf(q / width + a.eps);
-    if (lane == 0) {
-      if (a.mean) a.mean[row] = mean;
-      if (a.rstd) a.rstd[row] = rstd;
-    }
+    store_float<WIDE>(a.mean, row, lane == 0, mean);
+    store_float<WIDE>(a.rstd, row, lane == 0, rstd);
     T* y = static_cast<T*>(a.y) + row * a.ldy;
     each_piece<NC>([&](auto c, auto last) __attribute__((always_inline)) {
       const int at = 8 * (lane + TL * c);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[c][e] *= rstd;
-      if (a.codes) {
+      if constexpr (KEEP) {
         // (past the end of a row of an infinite or NaN rstd there is no 0 but NaN: its block has that anyway)
         const uint32_t e = fa_block_exponent(fa_quad_most(v[c]));
-        if (!last || at < pitch) {
-          *reinterpret_cast<uint2*>(a.codes + row * pitch + at) = fa_codes8(v[c], e);
-          if ((lane & 3) == 0) a.exponents[row * epitch + (at >> 5)] = (uint8_t)e;
-        }
+        store_codes<WIDE, last>(a.codes + row * pitch, a.exponents + row * epitch, pitch, at, fa_codes8(v[c], e), e);
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[c][e] = v[c][e] * gamma[c][e] + beta[c][e];
@@ -282,16 +308,18 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_backw
   const float width = (float)D;
   const int64_t pitch = fa_code_pitch(D), epitch = fa_exponent_pitch(D);
   const int w = worker_of(ch.first, a.blocks.p, blockIdx.x);
-  const int64_t begin = a.blocks.row0[w] + (int64_t)(blockIdx.x - ch.first[w]) * ch.rows_per_chunk;
-  const int64_t end = min(begin + ch.rows_per_chunk, a.blocks.row0[w + 1]);
+  // (a worker's chunks take its rows in turn: rows that are read at one time lie together, and not one chunk apart, which
+  // for many widths would be the same few channels of the memory)
+  const int64_t begin = a.blocks.row0[w] + (int64_t)(blockIdx.x - ch.first[w]) * TEAMS, end = a.blocks.row0[w + 1];
+  const int64_t step = (int64_t)(ch.first[w + 1] - ch.first[w]) * TEAMS;
   constexpr bool WIDE = L == 64;
   const T* dy = static_cast<const T*>(a.dy);
   const T* x = static_cast<const T*>(a.x);
   const T* residual = static_cast<const T*>(a.residual);
-  raw8<T> next_dy[NC], next_x[KEPT ? 1 : NC], next_res[NC];
+  raw8<T> next_dy[NC], next_x[KEPT ? 1 : NC];
   uint2 next_codes[KEPT ? NC : 1];
   uint32_t next_e[KEPT ? NC : 1];
-  uint32_t last_dy = 0, last_x = 0, last_res = 0;
+  uint32_t last_dy = 0, last_x = 0;
   float next_mean = 0.f, next_rstd = 0.f;
   auto load = [&](int64_t row) __attribute__((always_inline)) {
     next_rstd = a.rstd[row];
@@ -307,9 +335,9 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_backw
           const __amdgpu_buffer_rsrc_t codes =
               __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(a.codes) + row * pitch, 0, (int)pitch, 0x00020000);
           const __amdgpu_buffer_rsrc_t exponents =
-              __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.exponents) + row * epitch, 0, (int)pitch / 32, 0x00020000);
+              __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.exponents) + row * epitch, 0, (int)epitch, 0x00020000);
           next_codes[c] = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(codes, at, 0, 0));
-          next_e[c] = __builtin_amdgcn_raw_buffer_load_b8(exponents, at >> 5, 0, 0);
+          next_e[c] = __builtin_amdgcn_raw_buffer_load_b32(exponents, at >> 5 & ~3, 0, 0);
         } else {
           next_codes[c] = make_uint2(0u, 0u);
           next_e[c] = 0u;
@@ -325,12 +353,6 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_backw
 #pragma unroll
       for (int c = 0; c < NC; ++c) next_x[c] = from.load(8 * (lane + TL * c), D);
       last_x = from.last();
-    }
-    if (residual) {
-      const row_in<WIDE, T> more(residual + row * a.ldr, D);
-#pragma unroll
-      for (int c = 0; c < NC; ++c) next_res[c] = more.load(8 * (lane + TL * c), D);
-      last_res = more.last();
     }
   };
   int team = threadIdx.x / TL;
@@ -349,26 +371,41 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_backw
     }
   }
   int turn = 0;
-  for (; row < end; row += TEAMS, turn ^= 1) {
-    const float rstd = next_rstd, mean = next_mean;
+  for (; row < end; row += step, turn ^= 1) {
+    // (copied here and not where the next one arrives, which would be a wait for it)
+    float rstd;
+    asm volatile("v_mov_b32 %0, %1" : "=v"(rstd) : "v"(next_rstd));
+    const float mean = next_mean;
     float xh[NC][8], h[NC][8];
     raw8<T> res[NC];
+    uint32_t last_res = 0;
+    // the residual is wanted at the end of the row: this one's
+    if (WIDE || residual) {
+      const row_in<WIDE, T> more(residual ? residual + row * a.ldr : nullptr, D);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) res[c] = more.load(8 * (lane + TL * c), D);
+      last_res = more.last();
+    }
     // (what lies past the end of the row is zero in h, and so adds nothing)
-    const uint32_t end_res = last_res;
     each_piece<NC>([&](auto c, auto last) __attribute__((always_inline)) {
       const int at = 8 * (lane + TL * c);
       values<WIDE, last>(next_dy[c], last_dy, at, D, h[c]);
       if constexpr (KEPT) {
         asm("" : "+v"(next_codes[c].x), "+v"(next_codes[c].y), "+v"(next_e[c]));
-        fa_values8(next_codes[c], fa_block_scale(next_e[c]), xh[c]);
+        uint32_t e = next_e[c];
+        if constexpr (WIDE) {            // the byte of the word; what is past the last block is not written there
+          e = e >> (at >> 2 & 24) & 255u;
+          if constexpr (last) e = at < pitch ? e : 0u;
+        }
+        fa_values8(next_codes[c], fa_block_scale(e), xh[c]);
       } else {
         values<WIDE, last>(next_x[c], last_x, at, D, xh[c]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) xh[c][e] = (xh[c][e] - mean) * rstd;
       }
-      if (residual) res[c] = next_res[c];
     });
-    load(row + TEAMS < end ? row + TEAMS : row);
+    load(row + step < end ? row + step : row);
+    __builtin_amdgcn_sched_barrier(0);
     float s = 0.f, q = 0.f;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
@@ -400,9 +437,9 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_backw
       const int at = 8 * (lane + TL * c);
 #pragma unroll
       for (int e = 0; e < 8; ++e) h[c][e] = rstd * (h[c][e] - s - xh[c][e] * q);
-      if (residual) {
+      if (WIDE || residual) {
         float r[8];
-        values<WIDE, last>(res[c], end_res, at, D, r);
+        values<WIDE, last>(res[c], last_res, at, D, r);
 #pragma unroll
         for (int e = 0; e < 8; ++e) h[c][e] += r[e];
       }
@@ -537,7 +574,9 @@ void norm(const fa_norm_args& a, hipStream_t st) {
   const int teams = W > 1 ? 1 : kThreads / L;
   int64_t blocks = (a.rows + teams - 1) / teams;
   if (blocks > 2048) blocks = 2048;
-  hipLaunchKernelGGL((fa_layer_norm_kernel<T, L, NC, W>), dim3((unsigned)blocks), dim3(W > 1 ? 64 * W : kThreads), 0, st, a);
+  const dim3 grid((unsigned)blocks), block(W > 1 ? 64 * W : kThreads);
+  if (a.codes) hipLaunchKernelGGL((fa_layer_norm_kernel<T, true, L, NC, W>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((fa_layer_norm_kernel<T, false, L, NC, W>), grid, block, 0, st, a);
 }
 
 // The team of a width: no more lanes than the row has work for, all pieces but the last whole.

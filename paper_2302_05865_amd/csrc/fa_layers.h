@@ -167,7 +167,6 @@ __device__ __forceinline__ uint32_t fa_quad_most(const float v[8]) {
   return m;
 }
 __device__ __forceinline__ uint2 fa_codes8(const float v[8], uint32_t e) {
-  if (e == 255u) return make_uint2(0u, 0u);
   const float inverse = __uint_as_float((254u - e) << 23);
   uint32_t w[2] = {0u, 0u};
 #pragma unroll
@@ -175,7 +174,7 @@ __device__ __forceinline__ uint2 fa_codes8(const float v[8], uint32_t e) {
     const int c = (int)fminf(fmaxf(rintf(v[k] * inverse), -127.f), 127.f);
     w[k >> 2] |= ((uint32_t)c & 255u) << (8 * (k & 3));
   }
-  return make_uint2(w[0], w[1]);
+  return e == 255u ? make_uint2(0u, 0u) : make_uint2(w[0], w[1]);
 }
 __device__ __forceinline__ void fa_values8(uint2 codes, float scale, float v[8]) {
 #pragma unroll
