@@ -266,23 +266,27 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_kerne
 
 namespace {
 
-// Rows that one workgroup of the backward pass takes: a share of one worker's.  About kNormBlocks workgroups in all, three
-// for every compute unit, which is what their registers allow.
+// Rows that one workgroup of the backward pass takes: a share of one worker's.  There are no more chunks than workgroups
+// have registers for at one time, three for every compute unit: a few that wait for a second turn would double the time.
 constexpr int kNormBlocks = 768;
 
 struct norm_chunks {
   int first[FA_P_MAX + 1];   // worker w has the chunks [first[w], first[w + 1])
-  int64_t rows_per_chunk;
 };
 
 norm_chunks cut(const fa_row_blocks& b, int64_t rows) {
   norm_chunks c;
-  c.rows_per_chunk = (rows + kNormBlocks - 1) / kNormBlocks;
-  if (c.rows_per_chunk < 4) c.rows_per_chunk = 4;
-  c.first[0] = 0;
-  for (int w = 0; w < FA_P_MAX; ++w)
-    c.first[w + 1] = c.first[w] + (w < b.p ? (int)((b.row0[w + 1] - b.row0[w] + c.rows_per_chunk - 1) / c.rows_per_chunk) : 0);
-  return c;
+  int64_t share = (rows + kNormBlocks - 1) / kNormBlocks;
+  if (share < 4) share = 4;
+  for (;; share += share / 16 + 1) {
+    int64_t chunks = 0;
+    c.first[0] = 0;
+    for (int w = 0; w < FA_P_MAX; ++w) {
+      if (w < b.p) chunks += (b.row0[w + 1] - b.row0[w] + share - 1) / share;
+      c.first[w + 1] = (int)chunks;
+    }
+    if (chunks <= kNormBlocks) return c;      // (at the latest with one chunk a worker)
+  }
 }
 
 // the worker that chunk k belongs to: as many workers end at or before it as come ahead of it
