@@ -13,32 +13,53 @@ from ._binding import _check, load_library
 from ._ctypes_defs import FA_BF16, FA_CHECKPOINT_BLOCK, FA_ERR_ARG, FA_F32, FA_P_MAX
 
 
+# What every call needs of torch and the library, looked up at the first one: small calls cost as much as their launches and
+# what is done here.
+torch = None
+_CODES: dict = {}
+_raw_stream = None
+_lib = None
+
+
+def _ready() -> None:
+    global torch, _CODES, _raw_stream, _lib
+    if _lib is not None:
+        return
+    import torch as _torch
+    torch = _torch
+    _CODES = {_torch.float32: FA_F32, _torch.bfloat16: FA_BF16}
+    _raw_stream = getattr(_torch._C, "_cuda_getCurrentRawStream", None)
+    if _raw_stream is None:
+        def _raw_stream(index):
+            return _torch.cuda.current_stream(index).cuda_stream
+    _lib = load_library()
+
+
 def _dtype(t, name: str) -> int:
-    import torch
-    if t.dtype == torch.float32:
-        return FA_F32
-    if t.dtype == torch.bfloat16:
-        return FA_BF16
-    raise TypeError(f"{name} must be float32 or bfloat16")
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32 or bfloat16")
+    return code
 
 
 def _matrix(t, name: str, shape=None, like=None):
     """A [rows, width] device tensor with unit inner stride: (address, leading dimension)."""
-    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.numel() and t.stride(1) != 1):
+    size, stride = t.shape, t.stride()
+    if not t.is_cuda or len(size) != 2 or (stride[1] != 1 and size[1] > 1 and size[0] > 0):
         raise TypeError(f"{name} must be a two-dimensional device tensor with unit inner stride")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and size != shape:
         raise TypeError(f"{name} must have shape {tuple(shape)}")
     if like is not None and (t.dtype != like.dtype or t.device != like.device):
         raise TypeError(f"{name} must have the type and device of the other activations")
-    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+    if size[0] > 1 and stride[0] < size[1]:
         raise TypeError(f"{name}: rows must not overlap")
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), stride[0]
 
 
 def _vector(t, name: str, n: int, device, dtype=None):
     if t is None:
         return None
-    if t.device != device or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
+    if t.device != device or t.shape != (n,) or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
         raise TypeError(f"{name} must be a contiguous vector of {n} elements on {device}"
                         + (f" of {dtype}" if dtype is not None else ""))
     return t.data_ptr()
@@ -46,38 +67,33 @@ def _vector(t, name: str, n: int, device, dtype=None):
 
 def _params(gamma, beta, n: int, device):
     """(gamma, beta, their type): both in one type."""
-    if gamma is not None and beta is not None and gamma.dtype != beta.dtype:
+    if gamma is None:
+        return None, _vector(beta, "beta", n, device), FA_F32 if beta is None else _dtype(beta, "gamma and beta")
+    if beta is not None and gamma.dtype != beta.dtype:
         raise TypeError("gamma and beta must have the same type")
-    one = gamma if gamma is not None else beta
-    return (_vector(gamma, "gamma", n, device), _vector(beta, "beta", n, device),
-            FA_F32 if one is None else _dtype(one, "gamma and beta"))
+    return _vector(gamma, "gamma", n, device), _vector(beta, "beta", n, device), _dtype(gamma, "gamma and beta")
 
 
 def _sizes(sizes: Sequence[int], rows: int):
-    sizes = [int(k) for k in sizes]
-    if not 1 <= len(sizes) <= FA_P_MAX:
+    p = len(sizes)
+    if not 1 <= p <= FA_P_MAX:
         raise TypeError(f"sizes must name 1 to {FA_P_MAX} workers")
+    sizes = [int(k) for k in sizes]
     if min(sizes) < 0 or sum(sizes) != rows:
         raise TypeError(f"sizes must be the workers' numbers of rows, {rows} in all")
-    return (ctypes.c_int64 * len(sizes))(*sizes), len(sizes)
+    return (ctypes.c_int64 * p)(*sizes), p
 
 
-class _On:
-    """The device of the call's tensors, current for the time of the call."""
-
-    def __init__(self, device):
-        import torch
-        self._torch, self._device, self._guard = torch, device, None
-
-    def __enter__(self):
-        if self._device.index != self._torch.cuda.current_device():
-            self._guard = self._torch.cuda.device(self._device)
-            self._guard.__enter__()
-        return self._torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self._guard is not None:
-            self._guard.__exit__(*exc)
+def _call(name: str, device, *args) -> None:
+    """The library's function on torch's current stream of the device that the tensors are on."""
+    index = device.index
+    if index == torch.cuda.current_device():
+        status = getattr(_lib, name)(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(device):
+            status = getattr(_lib, name)(*args, _raw_stream(index))
+    if status:
+        _check(status, name)
 
 
 class Checkpoint:
@@ -88,7 +104,7 @@ class Checkpoint:
     __slots__ = ("codes", "exponents", "features")
 
     def __init__(self, codes, exponents, features: int):
-        import torch
+        _ready()
         features = int(features)
         if features < 1:
             raise TypeError("features must be at least 1")
@@ -104,7 +120,7 @@ class Checkpoint:
 
     @classmethod
     def empty(cls, rows: int, features: int, device="cuda") -> "Checkpoint":
-        import torch
+        _ready()
         rows, features = int(rows), int(features)
         if rows < 0 or features < 1:
             raise TypeError("rows must be at least 0 and features at least 1")
@@ -134,20 +150,20 @@ def _apart(out, name: str, *others) -> None:
 
 def fa_checkpoint_pack(x, out: Optional[Checkpoint] = None) -> Checkpoint:
     """``x`` [rows, features] in 8 bits."""
+    _ready()
     ptr, ld = _matrix(x, "x")
     rows, features = x.shape
+    dtype, device = _dtype(x, "x"), x.device
     if out is None:
-        out = Checkpoint.empty(rows, features, x.device)
-    codes, exponents = out._for(rows, features, x.device)
-    with _On(x.device) as stream:
-        _check(load_library().fa_checkpoint_pack(ptr, ld, rows, features, _dtype(x, "x"), codes, exponents, stream),
-               "fa_checkpoint_pack")
+        out = Checkpoint.empty(rows, features, device)
+    codes, exponents = out._for(rows, features, device)
+    _call("fa_checkpoint_pack", device, ptr, ld, rows, features, dtype, codes, exponents)
     return out
 
 
 def fa_checkpoint_unpack(checkpoint: Checkpoint, dtype=None, out=None):
     """The values of a checkpoint as a [rows, features] tensor of ``dtype`` (default float32)."""
-    import torch
+    _ready()
     rows, features = checkpoint.rows, checkpoint.features
     device = checkpoint.codes.device
     if out is None:
@@ -156,9 +172,7 @@ def fa_checkpoint_unpack(checkpoint: Checkpoint, dtype=None, out=None):
         raise TypeError(f"out must be of {dtype}")
     ptr, ld = _matrix(out, "out", (rows, features))
     codes, exponents = checkpoint._for(rows, features, out.device)
-    with _On(device) as stream:
-        _check(load_library().fa_checkpoint_unpack(codes, exponents, rows, features, _dtype(out, "out"), ptr, ld, stream),
-               "fa_checkpoint_unpack")
+    _call("fa_checkpoint_unpack", device, codes, exponents, rows, features, _dtype(out, "out"), ptr, ld)
     return out
 
 
@@ -167,24 +181,26 @@ def fa_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, checkpoint: Optio
     """``(y, mean, rstd)`` of the layer norm of every row of ``x`` [rows, features].  ``checkpoint``
     (``Checkpoint.empty(rows, features)``) receives the normalised rows, before gamma and beta, in
     8 bits.  ``stats=False``: mean and rstd are not wanted, and None."""
-    import torch
+    _ready()
     ptr, ld = _matrix(x, "x")
     rows, features = x.shape
-    device = x.device
+    dtype, device = _dtype(x, "x"), x.device
     g, b, param_dtype = _params(gamma, beta, features, device)
     if out is None:
         out = torch.empty((rows, features), dtype=x.dtype, device=device)
-    yptr, ldy = _matrix(out, "out", (rows, features), x)
-    _apart(out, "out", x)
-    codes, exponents = checkpoint._for(rows, features, device) if checkpoint is not None else (None, None)
-    mean = rstd = None
+        yptr, ldy = out.data_ptr(), features
+    else:
+        yptr, ldy = _matrix(out, "out", (rows, features), x)
+        _apart(out, "out", x)
+    codes = exponents = mean = rstd = mptr = rptr = None
+    if checkpoint is not None:
+        codes, exponents = checkpoint._for(rows, features, device)
     if stats:
-        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=device)
-    with _On(device) as stream:
-        _check(load_library().fa_layer_norm(
-            ptr, ld, rows, features, _dtype(x, "x"), g, b, param_dtype, float(eps), yptr, ldy,
-            mean.data_ptr() if stats else None, rstd.data_ptr() if stats else None, codes, exponents, stream),
-            "fa_layer_norm")
+        mean = torch.empty(rows, dtype=torch.float32, device=device)
+        rstd = torch.empty(rows, dtype=torch.float32, device=device)
+        mptr, rptr = mean.data_ptr(), rstd.data_ptr()
+    _call("fa_layer_norm", device, ptr, ld, rows, features, dtype, g, b, param_dtype, eps, yptr, ldy, mptr, rptr, codes,
+          exponents)
     return out, mean, rstd
 
 
@@ -193,25 +209,28 @@ def fa_layer_norm_backward(dy, rstd, sizes: Sequence[int], dgamma=None, dbeta=No
     """dx of the layer norm, and in place every worker's ``dgamma[w]`` and ``dbeta[w]`` ([p, features],
     usually slices of G's rows).  ``sizes[w]``: rows of worker w.  The normalised rows come from the
     ``checkpoint`` or from ``x`` and ``mean``.  ``residual`` is added to dx."""
-    import torch
+    _ready()
     ptr, ld = _matrix(dy, "dy")
-    rows, features = dy.shape
-    device = dy.device
+    shape = dy.shape
+    rows, features = shape
+    dtype, device = _dtype(dy, "dy"), dy.device
     sz, p = _sizes(sizes, rows)
     if (x is None) == (checkpoint is None) or (x is not None and mean is None):
         raise TypeError("the normalised rows come from x and mean, or from checkpoint")
-    xptr, ldx = _matrix(x, "x", (rows, features), dy) if x is not None else (None, 0)
-    rptr, ldr = _matrix(residual, "residual", (rows, features), dy) if residual is not None else (None, 0)
+    if rstd is None:
+        raise TypeError("rstd must be given")
+    xptr, ldx = _matrix(x, "x", shape, dy) if x is not None else (None, 0)
+    rptr, ldr = _matrix(residual, "residual", shape, dy) if residual is not None else (None, 0)
     codes, exponents = checkpoint._for(rows, features, device) if checkpoint is not None else (None, None)
     g, _, param_dtype = _params(gamma, None, features, device)
     mptr = _vector(mean, "mean", rows, device, torch.float32)
     sptr = _vector(rstd, "rstd", rows, device, torch.float32)
-    if sptr is None:
-        raise TypeError("rstd must be given")
     if out is None:
-        out = torch.empty((rows, features), dtype=dy.dtype, device=device)
-    optr, ldo = _matrix(out, "out", (rows, features), dy)
-    _apart(out, "out", dy, x, residual)
+        out = torch.empty(shape, dtype=dy.dtype, device=device)
+        optr, ldo = out.data_ptr(), features
+    else:
+        optr, ldo = _matrix(out, "out", shape, dy)
+        _apart(out, "out", dy, x, residual)
     grad, dgptr, lddg, dbptr, lddb = None, None, 0, None, 0
     if dgamma is not None:
         dgptr, lddg = _matrix(dgamma, "dgamma", (p, features))
@@ -219,18 +238,18 @@ def fa_layer_norm_backward(dy, rstd, sizes: Sequence[int], dgamma=None, dbeta=No
     if dbeta is not None:
         dbptr, lddb = _matrix(dbeta, "dbeta", (p, features), dgamma)
         grad = dbeta
-    if grad is not None and grad.device != device:
-        raise TypeError("dgamma and dbeta must be on the device of dy")
-    lib = load_library()
-    with _On(device) as stream:
-        need = lib.fa_layer_norm_backward_workspace(sz, p, features) if grad is not None else 0
+    need, space, grad_dtype = 0, None, FA_F32
+    if grad is not None:
+        if grad.device != device:
+            raise TypeError("dgamma and dbeta must be on the device of dy")
+        grad_dtype = _dtype(grad, "dgamma and dbeta")
+        need = _lib.fa_layer_norm_backward_workspace(sz, p, features)
         if need < 0:
             _check(FA_ERR_ARG, "fa_layer_norm_backward_workspace")
-        space = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-        _check(lib.fa_layer_norm_backward(
-            ptr, ld, sz, p, features, _dtype(dy, "dy"), xptr, ldx, mptr, sptr, codes, exponents, g, param_dtype, rptr, ldr,
-            optr, ldo, dgptr, lddg, dbptr, lddb, _dtype(grad, "dgamma and dbeta") if grad is not None else FA_F32,
-            space.data_ptr() if need else None, need, stream), "fa_layer_norm_backward")
+        if need:
+            space = torch.empty(need, dtype=torch.uint8, device=device)
+    _call("fa_layer_norm_backward", device, ptr, ld, sz, p, features, dtype, xptr, ldx, mptr, sptr, codes, exponents, g,
+          param_dtype, rptr, ldr, optr, ldo, dgptr, lddg, dbptr, lddb, grad_dtype, space.data_ptr() if need else None, need)
     return out
 
 
@@ -239,29 +258,26 @@ def fa_linear_grad(dy, checkpoint: Checkpoint, sizes: Sequence[int], dweight, db
     contiguous, usually slices of G's rows) and ``dbias[w]`` ([p, outputs]) of a linear layer from
     the gradient ``dy`` [rows, outputs] of its outputs and the checkpoint of its input.  With
     ``gamma`` and ``beta`` the layer's input was ``values * gamma + beta``."""
-    import torch
+    _ready()
     ptr, ld = _matrix(dy, "dy")
     rows, outputs = dy.shape
-    device, features = dy.device, checkpoint.features
+    dtype, device, features = _dtype(dy, "dy"), dy.device, checkpoint.features
     sz, p = _sizes(sizes, rows)
     codes, exponents = checkpoint._for(rows, None, device)
     if (gamma is None) != (beta is None):
         raise TypeError("gamma and beta go together")
     g, b, param_dtype = _params(gamma, beta, features, device)
-    if (not dweight.is_cuda or dweight.device != device or tuple(dweight.shape) != (p, outputs, features) or
-            (features > 1 and dweight.stride(2) != 1) or (outputs > 1 and dweight.stride(1) != features) or
-            (p > 1 and dweight.stride(0) < outputs * features)):
+    stride = dweight.stride()
+    if (dweight.device != device or dweight.shape != (p, outputs, features) or (features > 1 and stride[2] != 1) or
+            (outputs > 1 and stride[1] != features) or (p > 1 and stride[0] < outputs * features)):
         raise TypeError(f"dweight must be [{p}, {outputs}, {features}] on {device}, every worker's part contiguous")
     bptr, ldb = None, 0
     if dbias is not None:
         bptr, ldb = _matrix(dbias, "dbias", (p, outputs), dweight)
-    lib = load_library()
-    with _On(device) as stream:
-        need = lib.fa_linear_grad_workspace(sz, p, features, outputs, _dtype(dy, "dy"))
-        if need < 0:
-            _check(FA_ERR_ARG, "fa_linear_grad_workspace")
-        space = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-        _check(lib.fa_linear_grad(
-            ptr, ld, sz, p, features, outputs, _dtype(dy, "dy"), codes, exponents, g, b, param_dtype, dweight.data_ptr(),
-            dweight.stride(0), bptr, ldb, _dtype(dweight, "dweight"), space.data_ptr() if need else None, need, stream),
-            "fa_linear_grad")
+    need, space = _lib.fa_linear_grad_workspace(sz, p, features, outputs, dtype), None
+    if need < 0:
+        _check(FA_ERR_ARG, "fa_linear_grad_workspace")
+    if need:
+        space = torch.empty(need, dtype=torch.uint8, device=device)
+    _call("fa_linear_grad", device, ptr, ld, sz, p, features, outputs, dtype, codes, exponents, g, b, param_dtype,
+          dweight.data_ptr(), stride[0], bptr, ldb, _dtype(dweight, "dweight"), space.data_ptr() if need else None, need)
