@@ -395,7 +395,7 @@ fa_status fa_aggregate_static(const void* G, int64_t ldg, int p, int64_t n, int 
 #define FA_CHECKPOINT_BLOCK 32          /* features of a row that share a scale in a checkpoint */
 #define FA_FEATURES_MAX (1 << 18)       /* widest row of a checkpoint or linear layer */
 #define FA_NORM_FEATURES_MAX 16384      /* widest row of a layer norm */
-#define FA_ROWS_MAX ((int64_t)1 << 40)
+#define FA_ROWS_MAX ((int64_t)1 << 36)  /* rows of all workers together */
 
 /*
  * An activation checkpoint in 8 bits: [rows, features] as codes (int8, rows of

@@ -98,8 +98,8 @@ __device__ __forceinline__ words<N> load_words(const unsigned char* p) {   // at
   __builtin_memcpy(&u, p, sizeof(u));
   return u;
 }
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const unsigned char* p) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(p), 0, 0x7fffffff, 0x00020000);
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const unsigned char* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(p), 0, bytes, 0x00020000);
 }
 template <int N>
 __device__ __forceinline__ words<N> buffer_words(__amdgpu_buffer_rsrc_t r, uint32_t lane, int row) {
@@ -176,16 +176,16 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
   const int64_t pitch = fa_code_pitch(a.features), epitch = fa_exponent_pitch(a.features);
 
   // The unit of dY and the unit of codes that this thread brings in: rows 8 piece.., columns.  Columns past the matrix
-  // take part like any other and are not written at the end, so all that matters is that what is read for them is
-  // there: a unit beyond the last column reads the tile's first one, one that the last column is in reads on into the
-  // next row.  The last rows of the whole matrix have no such next row: those, and steps that are not whole, are taken
-  // element by element behind the others.
+  // take part like any other and are not written at the end: what is read for them is the tile's first unit, or, where
+  // the last column is inside the unit, the next row's beginning.  A step is a buffer that ends with the last element of its
+  // last row: rows past the end come as zeros, and so does what would lie behind the matrix.  The end is kept in words of
+  // four bytes, in which the last column of an odd number of bf16 would be lost: there the last step is taken element by
+  // element behind the others.
   const int a_col = tid % (BM / AC) * AC, a_piece = tid / (BM / AC);
   const int b_col = tid % (BN / S::BC) * S::BC, b_piece = tid / (BN / S::BC);
-  const int64_t over = (AC - a.outputs % AC) % AC;        // elements of the last unit past the last column
-  const int64_t reach = a.blocks.row0[a.blocks.p] - (over + a.lddy - 1) / a.lddy;
-  const int64_t fast = a.lddy < (1 << 22) && min(end, reach) > begin ? (min(end, reach) - begin) / BK : 0;
   const int64_t steps = (end - begin + BK - 1) / BK;
+  const bool odd = sizeof(T) == 2 && (a.outputs & 1);
+  const int64_t fast = a.lddy >= (1 << 22) || steps == 0 ? 0 : odd ? steps - 1 : steps;
   const uint32_t a_off = (uint32_t)((int64_t)a_piece * 8 * a.lddy + (o0 + a_col < a.outputs ? a_col : 0)) * (uint32_t)sizeof(T);
   const int b_safe = i0 + b_col < pitch ? b_col : 0;
   const uint32_t b_off = (uint32_t)(b_piece * 8 * (int)pitch + b_safe);
@@ -212,10 +212,19 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
   const unsigned char* at_codes = reinterpret_cast<const unsigned char*>(a.codes) + begin * pitch + i0;
   const unsigned char* at_exponents = a.exponents + begin * epitch + (i0 >> 5);
   const int row_dy = (int)a.lddy * (int)sizeof(T), row_codes = (int)pitch, row_exponents = (int)epitch;
-  int64_t ahead = fast - 1;                               // steps to go on by: the last one is loaded again and again
-  // (part 0 and 1, half of the rows each; a step's own address goes on behind part 1)
+  // (ends of a step's buffers: of the last one's rows, of one row more than a step has where there is one more)
+  const int rows_last = (int)(end - begin - (steps - 1) * BK), wide_dy = (a.outputs - o0) * (int)sizeof(T);
+  const int last_dy = (rows_last - 1) * row_dy + wide_dy, full_dy = BK * row_dy + wide_dy;
+  const int last_codes = rows_last * row_codes - i0, full_codes = BK * row_codes;
+  const int last_exponents = rows_last * row_exponents - (i0 >> 5), full_exponents = BK * row_exponents;
+  const uint32_t step_dy = BK * row_dy, step_codes = BK * row_codes, step_exponents = BK * row_exponents;
+  int todo = (int)steps;                                  // steps from the one that is loaded next
+  // (part 0 and 1, half of the rows each; a step's own address goes on behind part 1, the last step comes again and again)
   auto load = [&](int part, AR (&ra)[8], BR (&rb)[8], uint32_t (&re)[8]) __attribute__((always_inline)) {
-    const __amdgpu_buffer_rsrc_t dy = buffer(at_dy), codes = buffer(at_codes), exponents = buffer(at_exponents);
+    const bool more = todo > 1;
+    const __amdgpu_buffer_rsrc_t dy = buffer(at_dy, more ? full_dy : last_dy),
+                                 codes = buffer(at_codes, more ? full_codes : last_codes),
+                                 exponents = buffer(at_exponents, more ? full_exponents : last_exponents);
 #pragma unroll
     for (int j = 4 * part; j < 4 * part + 4; ++j) {
       ra[j] = buffer_words<S::AW>(dy, a_off, j * row_dy);
@@ -223,11 +232,10 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
       re[j] = __builtin_amdgcn_raw_buffer_load_b8(exponents, e_off, j * row_exponents, 0);
     }
     if (part == 1) {
-      const int on = ahead > 0 ? BK : 0;
-      at_dy += (int64_t)on * row_dy;
-      at_codes += (int64_t)on * row_codes;
-      at_exponents += (int64_t)on * row_exponents;
-      --ahead;
+      at_dy += more ? step_dy : 0u;
+      at_codes += more ? step_codes : 0u;
+      at_exponents += more ? step_exponents : 0u;
+      todo -= more ? 1 : 0;
     }
   };
   // any step; rows past the end are zero, and nothing that is not there is read
