@@ -463,14 +463,26 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
   }
 }
 
+// n values `apart` from each other added up in their order, eight at a time on their way
+__device__ __forceinline__ float add_up(const float* p, int64_t apart, int n) {
+  float s = 0.f;
+  for (int q = 0; q < n; q += 8) {
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = q + e < n ? p[(q + e) * apart] : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += v[e];
+  }
+  return s;
+}
+
 // The splits of a worker's rows added up in their order, then as above.
 __global__ __launch_bounds__(kThreads) void fa_linear_grad_join_kernel(fa_linear_grad_args a) {
   const int64_t OI = (int64_t)a.outputs * a.features, all = OI + a.outputs;
   const int w = blockIdx.y;
   const float* part = a.partials + (int64_t)w * a.splits * all;
   for (int64_t k = (int64_t)blockIdx.x * kThreads + threadIdx.x; k < all; k += (int64_t)gridDim.x * kThreads) {
-    float s = 0.f;
-    for (int q = 0; q < a.splits; ++q) s += part[q * all + k];
+    float s = add_up(part + k, all, a.splits);
     if (k >= OI) {
       if (!a.dbias) continue;
       const int64_t at = w * a.lddbias + (k - OI);
@@ -481,8 +493,7 @@ __global__ __launch_bounds__(kThreads) void fa_linear_grad_join_kernel(fa_linear
     if (a.gamma) {
       const int64_t o = k / a.features;
       const int i = (int)(k - o * a.features);
-      float b = 0.f;
-      for (int q = 0; q < a.splits; ++q) b += part[q * all + OI + o];
+      const float b = add_up(part + OI + o, all, a.splits);
       const float gamma = a.param_bf16 ? fa_load1(static_cast<const fa_bf16*>(a.gamma) + i) : static_cast<const float*>(a.gamma)[i];
       const float beta = a.param_bf16 ? fa_load1(static_cast<const fa_bf16*>(a.beta) + i) : static_cast<const float*>(a.beta)[i];
       s = gamma * s + beta * b;
@@ -495,8 +506,18 @@ __global__ __launch_bounds__(kThreads) void fa_linear_grad_join_kernel(fa_linear
 
 namespace {
 
-// The two tiles of either type.  (outputs, features)
-constexpr int kWide[2][2] = {{128, 256}, {256, 256}}, kNarrow[2][2] = {{64, 128}, {128, 128}};
+// The two tiles of either type, and in how many parts the workers' rows are cut.  Time is counted in steps of a wide tile,
+// 2 us on a full card (bf16; 65536 x 4096 x 4096 takes 16 rounds of 64 of them): a narrow tile is a quarter of the
+// work, two of them share a compute unit, and the pair takes `step` of that (whole shapes: 65536 x 4096 x 4096 in 2.05 ms
+// wide, 2.86 ms narrow; fp32, 60 workers, 1001 -> 509: 0.164 and 0.184 ms).  A round of workgroups costs `more` beside its steps, for
+// the first loads and the last stores.  Parts are joined at the rate of memory, behind one more launch.
+struct tile_kind {
+  int outputs, features, slots;
+  float step, more;
+};
+constexpr tile_kind kTiles[2][2] = {{{128, 256, 256, 1.f, 5.f}, {64, 128, 512, 0.56f, 3.f}},     // fp32 dY: wide, narrow
+                                    {{256, 256, 256, 1.f, 5.f}, {128, 128, 512, 0.69f, 3.f}}};   // bf16 dY
+constexpr int kParts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
 
 struct plan {
   bool wide;
@@ -505,17 +526,25 @@ struct plan {
 };
 
 plan plan_of(const fa_row_blocks& b, int features, int outputs, int dtype) {
-  const int bf16 = dtype == FA_BF16;
-  int64_t most = 0;
-  for (int w = 0; w < b.p; ++w) most = b.row0[w + 1] - b.row0[w] > most ? b.row0[w + 1] - b.row0[w] : most;
-  auto tiles = [&](const int* t) { return (int64_t)((outputs + t[0] - 1) / t[0]) * ((features + t[1] - 1) / t[1]); };
-  plan c;
-  c.wide = tiles(kWide[bf16]) * b.p >= 200;
-  c.tiles = tiles(c.wide ? kWide[bf16] : kNarrow[bf16]);
-  int64_t s = 512 / (c.tiles * b.p);
-  if (s > most / 256) s = most / 256;
-  c.splits = s < 1 ? 1 : (int)s;
-  return c;
+  const int64_t mean = (b.row0[b.p] + b.p - 1) / b.p, steps = (mean + 63) / 64;
+  const double results = (double)b.p * outputs * features;
+  plan best = {};
+  double least = 0;
+  for (int narrow = 0; narrow < 2; ++narrow) {
+    const tile_kind& t = kTiles[dtype == FA_BF16][narrow];
+    const int64_t tiles = (int64_t)((outputs + t.outputs - 1) / t.outputs) * ((features + t.features - 1) / t.features);
+    for (const int parts : kParts) {
+      if (parts > 1 && parts > steps) break;
+      const int64_t rounds = (tiles * b.p * parts + t.slots - 1) / t.slots;
+      double cost = (double)rounds * ((double)((steps + parts - 1) / parts) * t.step + t.more);
+      if (parts > 1) cost += 1.5 + results * parts * (8 / 5.1e6 / 2);
+      if (best.splits == 0 || cost < least) {
+        least = cost;
+        best = {narrow == 0, parts, tiles};
+      }
+    }
+  }
+  return best;
 }
 
 }  // namespace
