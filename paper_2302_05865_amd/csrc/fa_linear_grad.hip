@@ -21,12 +21,10 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // x = h + m + l exactly, each with eight significant bits, h and m cut off (h of the largest finite value stays finite).
-// An infinity or a NaN is h, with nothing left over.
+// An infinity is h, with nothing left over; of a NaN, whatever h is, m is one.
 __device__ __forceinline__ void split3(float x, uint32_t* h, uint32_t* m, uint32_t* l) {
-  const uint32_t u = __float_as_uint(x);
-  const bool finite = (u & 0x7f800000u) != 0x7f800000u;
-  const uint32_t hu = (u & 0xffff0000u) | ((u & 0x7fffffffu) > 0x7f800000u ? 0x00400000u : 0u);
-  const float r = finite ? x - __uint_as_float(hu) : 0.f;
+  const uint32_t hu = __float_as_uint(x) & 0xffff0000u;
+  const float left = x - __uint_as_float(hu), r = __builtin_amdgcn_classf(x, 0x204) ? 0.f : left;
   const uint32_t mu = __float_as_uint(r) & 0xffff0000u;
   *h = hu;
   *m = mu;
@@ -343,8 +341,8 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
       }
     }
   };
-  // vector instructions of a quarter: 20 for a column of codes, 4 or 88 for one of dY, 4 for each column sum
-  constexpr int kVector = S::BC / 4 * 20 + S::AC * (S::PLANES == 1 ? 4 : 88) / 4 + S::PLANES * HM * 4;
+  // vector instructions of a quarter: 20 for a column of codes, 4 or 60 for one of dY, 4 for each column sum
+  constexpr int kVector = S::BC / 4 * 20 + S::AC * (S::PLANES == 1 ? 4 : 60) / 4 + S::PLANES * HM * 4;
   bf16x8 fa[2][S::PLANES][FM], fb[2][FN];
   if (fast > 0) {
     // A step k in half k % 2 of LDS takes four regions of 16 rows.  In the first three the last quarters of step k + 1 are
