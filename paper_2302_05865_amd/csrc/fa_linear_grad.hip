@@ -127,7 +127,9 @@ __device__ __forceinline__ words<N> load_some(const float* p, int valid) {
 
 // A wavefront issues in order: what is not a product goes between the products, a few instructions behind each, and costs
 // nothing there.  PRODUCTS matrix instructions, READS and WRITES of LDS and the vector instructions of a region.
-template <int PRODUCTS, int READS, int WRITES, int VECTOR, int I = 0>
+// (READS first, two behind a product, then the writes: nothing tells the compiler that those go to the other half.  Of the
+// WRITES, the LATE last ones are of dY in three pieces, and wait for most of the vector instructions.)
+template <int PRODUCTS, int READS, int WRITES, int LATE, int VECTOR, int I = 0>
 __device__ __forceinline__ void interleave() {
   if constexpr (I < PRODUCTS) {
     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                                        // a product
@@ -135,11 +137,12 @@ __device__ __forceinline__ void interleave() {
     __builtin_amdgcn_sched_group_barrier(0x020, 2, 0);                                        // loads from memory
     constexpr int V = VECTOR * (I + 1) / PRODUCTS - VECTOR * I / PRODUCTS;
     if constexpr (V > 0) __builtin_amdgcn_sched_group_barrier(0x002, V, 0);
-    // (writes behind all reads: nothing tells the compiler that they go to the other half)
-    constexpr int FROM = READS / 2, OVER = PRODUCTS - FROM > 0 ? PRODUCTS - FROM : 1, J = I - FROM;
-    constexpr int W = J < 0 ? 0 : WRITES * (J + 1) / OVER - WRITES * J / OVER;
-    if constexpr (W > 0) __builtin_amdgcn_sched_group_barrier(0x200, W, 0);
-    interleave<PRODUCTS, READS, WRITES, VECTOR, I + 1>();
+    constexpr int FROM = READS / 2, EARLY = WRITES - LATE, LAST = LATE > 0 ? PRODUCTS / 2 : PRODUCTS;
+    constexpr int OVER = LAST - FROM > 0 ? LAST - FROM : 1, J = I - FROM < OVER ? I - FROM : OVER - 1;
+    constexpr int W = J < 0 || I >= LAST ? 0 : EARLY * (J + 1) / OVER - EARLY * J / OVER;
+    constexpr int W_LATE = LATE == 0 ? 0 : I == PRODUCTS - 1 ? LATE - LATE / 2 : I == PRODUCTS - 2 ? LATE / 2 : 0;
+    if constexpr (W + W_LATE > 0) __builtin_amdgcn_sched_group_barrier(0x200, W + W_LATE, 0);
+    interleave<PRODUCTS, READS, WRITES, LATE, VECTOR, I + 1>();
   }
 }
 
@@ -268,8 +271,7 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
     get_b[y] = 2 * S::A_BYTES + jb * S::ROW + ((piece ^ swizzle(jb)) << 4);
   }
   // a quarter (of four) of a step's registers into LDS
-  auto stage = [&](int quarter, int half, const AR (&ra)[8], const BR (&rb)[8],
-                   const uint32_t (&re)[8]) __attribute__((always_inline)) {
+  auto stage_dy = [&](int quarter, int half, const AR (&ra)[8]) __attribute__((always_inline)) {
 #pragma unroll
     for (int c = quarter * AC / 4; c < (quarter + 1) * AC / 4; ++c) {
       unsigned char* at = lds + put_a[c >> 1] + (half * S::A_BYTES + c * S::ROW);
@@ -290,6 +292,8 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
 #pragma unroll
       for (int q = 0; q < S::PLANES; ++q) *reinterpret_cast<fa_u32x4*>(at + q * (BM * S::ROW)) = u[q];
     }
+  };
+  auto stage_codes = [&](int quarter, int half, const BR (&rb)[8], const uint32_t (&re)[8]) __attribute__((always_inline)) {
 #pragma unroll
     for (int c = quarter * S::BC / 4; c < (quarter + 1) * S::BC / 4; ++c) {
       fa_u32x4 u;
@@ -301,6 +305,12 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
       }
       *reinterpret_cast<fa_u32x4*>(lds + put_b[c >> 1] + (half * S::B_BYTES + c * S::ROW)) = u;
     }
+  };
+  auto stage = [&](int quarter, int half, const AR (&ra)[8], const BR (&rb)[8],
+                   const uint32_t (&re)[8]) __attribute__((always_inline)) {
+    if constexpr (S::PLANES == 1) stage_dy(quarter, half, ra);      // (fp32 pieces take long: last)
+    stage_codes(quarter, half, rb, re);
+    if constexpr (S::PLANES == 3) stage_dy(quarter, half, ra);
   };
   // the operands of 16 rows of a step, and their products
   auto fetch = [&](int half, int kk, bf16x8 (&fa)[S::PLANES][FM], bf16x8 (&fb)[FN]) __attribute__((always_inline)) {
@@ -377,7 +387,8 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
           multiply(fa[kk & 1], fb[kk & 1]);
           if (kk + 1 < KK) stage(kk + 1, 1 - half, raw_a[1 - half], raw_b[1 - half], raw_e[1 - half]);
           else stage(0, half, raw_a[half], raw_b[half], raw_e[half]);
-          interleave<S::PLANES * FM * FN, S::PLANES * FM + FN, (S::PLANES * S::AC + S::BC) / 4, kVector>();
+          interleave<S::PLANES * FM * FN, S::PLANES * FM + FN, (S::PLANES * S::AC + S::BC) / 4,
+                     S::PLANES == 3 ? S::PLANES * S::AC / 4 : 0, kVector>();
           __builtin_amdgcn_sched_barrier(0);
         }
       }
