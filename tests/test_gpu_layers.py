@@ -493,3 +493,30 @@ def test_refusals():
         fa_layer_norm(torch.zeros(2, 16385, device="cuda"))
     with pytest.raises(FaError):
         fa_layer_norm(x, eps=-1.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_far_apart(dtype):
+    """Rows of dy and dx four million elements apart: offsets inside a tile and a matrix pass 32 bits."""
+    announce("rows far apart", dtype)
+    rows, width, apart = 66 if dtype == "f32" else 130, 24, (1 << 23) + 1
+    rng = _rng(3, _seed_of(dtype))
+    flat = torch.zeros(rows * apart, dtype=TYPES[dtype], device="cuda")
+    dy = flat.view(rows, apart)[:, :width]
+    dy.copy_(torch.from_numpy(rng.normal(size=(rows, width))))
+    x = torch.from_numpy(rng.normal(size=(rows, 40))).float().cuda()
+    kept = fa_checkpoint_pack(x)
+    dw, db = torch.empty((2, width, 40), device="cuda"), torch.empty((2, width), device="cuda")
+    fa_linear_grad(dy, kept, [rows - 3, 3], dw, db)
+    other, ob = torch.empty_like(dw), torch.empty_like(db)
+    fa_linear_grad(dy.contiguous(), kept, [rows - 3, 3], other, ob)
+    v = lo.unpack(kept.codes.cpu().numpy(), kept.exponents.cpu().numpy(), 40)
+    want, wb = lo.linear_grad(_host(dy), v, [rows - 3, 3])
+    for got, b in ((dw, db), (other, ob)):
+        assert np.allclose(_host(got), want, rtol=0, atol=1e-4) and np.allclose(_host(b), wb, rtol=0, atol=1e-4)   # |terms| < 20 x 130
+    y, mean, rstd = fa_layer_norm(dy)
+    z, m, r = fa_layer_norm(dy.contiguous())
+    assert torch.equal(y, z) and torch.equal(mean, m) and torch.equal(rstd, r)
+    dx = fa_layer_norm_backward(dy, rstd, [rows], x=dy.contiguous(), mean=mean)
+    again = flat.view(rows, apart)[:, width:2 * width]
+    assert fa_layer_norm_backward(dy, rstd, [rows], x=dy, mean=mean, out=again) is again and torch.equal(dx, again)
