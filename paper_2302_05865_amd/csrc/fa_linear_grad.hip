@@ -157,6 +157,14 @@ __device__ __forceinline__ float add8(bf16x8 v, float s) {
 
 }  // namespace
 
+// What bounds it: the matrix core, at the clock that the card's power leaves it (1.8 to 2.1 GHz under this load), with the
+// issue of everything else between the products.  A wavefront makes 128 x 128 results, 16 products for 8 reads of LDS; with
+// 64 x 128 (tiles of 128 x 256) 65536 x 4096 x 4096 takes 2.59 ms, with 64 x 64 (two workgroups of 128 x 128 a compute
+// unit) 2.86 ms, so 2.05 ms = 1.07 PFLOP/s, which is what one plain product of such matrices per worker takes in a library.
+// Of that, turning and writing tiles to LDS is 0.5 ms, loads 0.4, column sums 0.1.
+// Few steps: 15 x 1024 rows of 768 -> 2304, bf16 to fp32, 90 us = 0.60 PFLOP/s, in 405 tiles for 256 compute units; the results
+// are 106 MB that are written at one time at the end of a tile (65 us without it).  fp32 dY, three products for one: 60
+// uneven workers, 30011 rows of 1001 -> 509, 139 us = 0.22 PFLOP/s, 0.66 with the pieces.  7 x 32 rows of 48 -> 64: 7.2 us.
 template <typename T, int BM, int BN, int BK>
 __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_grad_args a) {
   using S = tile<T, BM, BN, BK>;
@@ -485,7 +493,8 @@ __device__ __forceinline__ float add_up(const float* p, int64_t apart, int n) {
   return s;
 }
 
-// The splits of a worker's rows added up in their order, then as above.
+// The splits of a worker's rows added up in their order, then as above.  Bound by memory (its parts are read once); eight
+// loads a thread in flight.
 __global__ __launch_bounds__(kThreads) void fa_linear_grad_join_kernel(fa_linear_grad_args a) {
   const int64_t OI = (int64_t)a.outputs * a.features, all = OI + a.outputs;
   const int w = blockIdx.y;
