@@ -174,10 +174,10 @@ __device__ __forceinline__ void each_piece(F f) {
 //
 // Bound by memory from some thousand rows on.  A row lies in registers from its one read to its one write, so the centred
 // sum of squares costs no second pass; the next row's loads stand ahead of this one's reductions, and nothing a wavefront
-// waits for is behind a branch (the waits would be for everything in flight: 65536 x 4096 bf16 230 us, 217 without).
-// Rows of 512 features and more are read and written as buffers of their own length, in which lanes past the end do nothing.
-// Measured: 65536 x 4096 bf16 217 us = 4.95 TB/s (a copy: 5.13), 15360 x 768 bf16 with a checkpoint 15.3 us = 3.9 TB/s, one row of
-// 768 2.9 us, which is a launch and one turn to memory and back.
+// waits for is behind a branch (the waits would be for everything in flight).
+// Rows of more than 256 features are read and written as buffers of their own length, in which lanes past the end do nothing.
+// Measured: 65536 x 4096 bf16 217 us = 4.95 TB/s (a copy: 5.13), 15360 x 768 bf16 with a checkpoint 15.3 us = 3.9 TB/s, one
+// row of 768 2.9 us, which is a launch and one turn to memory and back.
 template <typename T, bool KEEP, int L, int NC, int W>
 __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_kernel(fa_norm_args a) {
   static_assert(W == 1 || L == 64, "a team of several wavefronts uses all their lanes");

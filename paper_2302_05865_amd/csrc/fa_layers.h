@@ -149,8 +149,8 @@ __device__ __forceinline__ void fa_load8_param(const void* p, int bf16, int at, 
 // A block of 32 consecutive features of a row holds codes c and one byte e, and stands for c 2^(e - 127).  From the
 // largest |v| of the block, of binary exponent E: e - 127 = max(E - 6, -126), so |v| 2^(127 - e) is below 128 and exact,
 // c = that rounded to the nearest whole number (ties to even), at most 127 in size.  The value is off by at most half of
-// 2^(e - 127), by less than all of it where the code was held at 127; it has seven significant bits: exact in bf16.  A block with an infinity or a NaN has e = 255 and codes 0,
-// whose value, 0 times infinity, is NaN.
+// 2^(e - 127), by less than all of it where the code was held at 127; it has seven significant bits: exact in bf16.  A block
+// with an infinity or a NaN has e = 255 and codes 0, whose value, 0 times infinity, is NaN.
 __device__ __forceinline__ uint32_t fa_block_exponent(uint32_t most_bits) {   // bits of the largest |v|
   const uint32_t biased = most_bits >> 23;
   if (biased == 255u) return 255u;

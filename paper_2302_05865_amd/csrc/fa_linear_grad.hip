@@ -157,11 +157,12 @@ __device__ __forceinline__ float add8(bf16x8 v, float s) {
 
 }  // namespace
 
-// What bounds it: the matrix core, at the clock that the card's power leaves it (1.8 to 2.1 GHz under this load), with the
-// issue of everything else between the products.  A wavefront makes 128 x 128 results, 16 products for 8 reads of LDS; with
-// 64 x 128 (tiles of 128 x 256) 65536 x 4096 x 4096 takes 2.59 ms, with 64 x 64 (two workgroups of 128 x 128 a compute
-// unit) 2.86 ms, so 2.05 ms = 1.07 PFLOP/s, which is what one plain product of such matrices per worker takes in a library.
-// Of that, turning and writing tiles to LDS is 0.5 ms, loads 0.4, column sums 0.1.
+// What bounds it: in long workers, issue.  A SIMD has one wavefront (its results take half of the registers), which issues
+// 4.2 vector, 0.8 LDS and 1.1 other instructions for every product, in order: the matrix core is busy 51 % of the cycles (at
+// 2.0 GHz), the wavefront waits in 42 %.  A wavefront makes 128 x 128 results, 16 products for 8 reads of LDS: 65536 x
+// 4096 x 4096 in 2.05 to 2.11 ms = 1.04 to 1.07 PFLOP/s, as long as one plain product per worker in a library (2.08 ms); with
+// 64 x 128 (tiles of 128 x 256) 2.59 ms, with 64 x 64 (128 x 128, two workgroups a compute unit) 2.93.  At 2.16 ms it took
+// 1.57 without turning tiles and writing them, 1.69 without loads, 2.07 without column sums.
 // Few steps: 15 x 1024 rows of 768 -> 2304, bf16 to fp32, 90 us = 0.60 PFLOP/s, in 405 tiles for 256 compute units; the results
 // are 106 MB that are written at one time at the end of a tile (65 us without it).  fp32 dY, three products for one: 60
 // uneven workers, 30011 rows of 1001 -> 509, 139 us = 0.22 PFLOP/s, 0.66 with the pieces.  7 x 32 rows of 48 -> 64: 7.2 us.
@@ -527,8 +528,9 @@ namespace {
 // The two tiles of either type, and in how many parts the workers' rows are cut.  Time is counted in steps of a wide tile,
 // 2 us on a full card (bf16; 65536 x 4096 x 4096 takes 16 rounds of 64 of them): a narrow tile is a quarter of the
 // work, two of them share a compute unit, and the pair takes `step` of that (whole shapes: 65536 x 4096 x 4096 in 2.05 ms
-// wide, 2.86 ms narrow; fp32, 60 workers, 1001 -> 509: 0.164 and 0.184 ms).  A round of workgroups costs `more` beside its steps, for
-// the first loads and the last stores.  Parts are joined at the rate of memory, behind one more launch.
+// wide, 2.93 ms narrow; 15 workers of 1024 rows, 768 -> 2304: 0.089 and 0.108 ms; fp32, 60 workers, 1001 -> 509: 0.140 and
+// 0.164 ms).  A round of workgroups costs `more` beside its steps, for the first loads and the last stores.  Parts are
+// joined at the rate of memory, behind one more launch.
 struct tile_kind {
   int outputs, features, slots;
   float step, more;

@@ -497,9 +497,9 @@ def test_refusals():
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_rows_far_apart(dtype):
-    """Rows of dy and dx four million elements apart: offsets inside a tile and a matrix pass 32 bits."""
+    """Rows of dy and dx 2^24 elements apart: offsets in bytes inside a tile and a matrix pass 32 bits."""
     announce("rows far apart", dtype)
-    rows, width, apart = 66 if dtype == "f32" else 130, 24, (1 << 23) + 1
+    rows, width, apart = 66 if dtype == "f32" else 130, 24, (1 << 24) + 1
     rng = _rng(3, _seed_of(dtype))
     flat = torch.zeros(rows * apart, dtype=TYPES[dtype], device="cuda")
     dy = flat.view(rows, apart)[:, :width]
