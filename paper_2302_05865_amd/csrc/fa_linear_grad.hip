@@ -43,7 +43,8 @@ __device__ __forceinline__ uint32_t upper_halves(uint32_t a, uint32_t b) { retur
 // thread brings in 8 rows of a few outputs of dY and 8 rows of a few codes, and turns them on the way: LDS holds, for
 // every output (feature), the BK values of the contracted index in pieces of 8, which is what a lane of the matrix
 // instruction takes with one 16-byte read.  Piece c of column j lies at place c ^ swizzle(j): 16 lanes that read one
-// piece of 16 neighbouring columns, and 8 that write one piece of every eighth column, meet no bank twice.
+// piece of 16 neighbouring columns, and 8 that write one piece of every second, fourth or eighth column (as wide as a
+// thread's unit is), meet no bank twice.
 namespace {
 
 template <typename T, int BM, int BN, int BK>
@@ -59,7 +60,7 @@ struct tile {
   static_assert(BK == 64 && PIECES == 8, "swizzle() is for eight pieces");
 };
 
-__device__ __forceinline__ int swizzle(int column) { return ((column >> 1) ^ (column >> 3)) & 7; }
+__device__ __forceinline__ int swizzle(int column) { return ((column >> 1) ^ (column >> 4)) & 7; }
 
 __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");   // (loads from memory stay in flight)
@@ -263,9 +264,10 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
     }
   };
   // Places in LDS as a few addresses of the lane and constants.  With column j = 8 g + r, swizzle(j) = swizzle(8 g) ^ (r / 2):
-  // a unit's column 8 g + r is written at put[r / 2] + r ROW.  With j = j0 + 32 m, swizzle(j) = swizzle(j0) ^ 4 (m % 2):
-  // piece 2 kk + lane / 32 of it is read at get[kk ^ 2 (m % 2)] + 32 m ROW.  Of the two wavefronts that share their
-  // outputs, each adds up one half of them, the half that it takes first: its results are in the order turned by `turn`.
+  // a unit's column 8 g + r is written at put[r / 2] + r ROW.  With j = j0 + 32 m in a run of 32, 64 or 128 columns that
+  // begins at a multiple of its length, j0 in its first 32, swizzle(j) = swizzle(j0) ^ 2 m: piece 2 kk + lane / 32 of it is
+  // read at get[kk ^ m] + 32 m ROW.  Of the two wavefronts that share their outputs, each adds up one half of them, the
+  // half that it takes first: its results are in the order turned by `turn`.
   uint32_t put_a[4], put_b[4], get_first[4], get_last[4], get_b[4];
   const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
   const int turn = FM > 1 ? (wave & 1) * HM : 0;
@@ -325,13 +327,13 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
   auto fetch = [&](int half, int kk, bf16x8 (&fa)[S::PLANES][FM], bf16x8 (&fb)[FN]) __attribute__((always_inline)) {
 #pragma unroll
     for (int n = 0; n < FN; ++n)
-      fb[n] = *reinterpret_cast<const bf16x8*>(lds + get_b[kk ^ (2 * (n & 1))] + (half * S::B_BYTES + 32 * n * S::ROW));
+      fb[n] = *reinterpret_cast<const bf16x8*>(lds + get_b[kk ^ n] + (half * S::B_BYTES + 32 * n * S::ROW));
 #pragma unroll
     for (int q = 0; q < S::PLANES; ++q)
 #pragma unroll
       for (int m = 0; m < FM; ++m) {
         const int mm = m < HM ? m : m - HM;
-        const uint32_t at = m < HM ? get_first[kk ^ (2 * (mm & 1))] : get_last[kk ^ (2 * (mm & 1))];
+        const uint32_t at = m < HM ? get_first[kk ^ mm] : get_last[kk ^ mm];
         fa[q][m] = *reinterpret_cast<const bf16x8*>(lds + at + (half * S::A_BYTES + 32 * mm * S::ROW + q * (BM * S::ROW)));
       }
   };
