@@ -158,12 +158,13 @@ __device__ __forceinline__ float add8(bf16x8 v, float s) {
 
 }  // namespace
 
-// What bounds it: in long workers, issue.  A SIMD has one wavefront (its results take half of the registers), which issues
-// 4.2 vector, 0.8 LDS and 1.1 other instructions for every product, in order: the matrix core is busy 51 % of the cycles (at
-// 2.0 GHz), the wavefront waits in 42 %.  A wavefront makes 128 x 128 results, 16 products for 8 reads of LDS: 65536 x
-// 4096 x 4096 in 2.05 to 2.11 ms = 1.04 to 1.07 PFLOP/s, as long as one plain product per worker in a library (2.08 ms); with
-// 64 x 128 (tiles of 128 x 256) 2.59 ms, with 64 x 64 (128 x 128, two workgroups a compute unit) 2.93.  At 2.16 ms it took
-// 1.57 without turning tiles and writing them, 1.69 without loads, 2.07 without column sums.
+// What bounds it: in long workers, issue and what it waits for.  A SIMD has one wavefront (its results take half of the
+// registers), which issues 4.2 vector, 0.8 LDS and 1.1 other instructions for every product, in order: the matrix core is busy
+// 51 % of the cycles (at 2.0 GHz), the wavefront waits in 42 %.  A wavefront makes 128 x 128 results, 16 products for 8 reads
+// of LDS: 65536 x 4096 x 4096 in 2.04 to 2.11 ms = 1.04 to 1.08 PFLOP/s, as long as one plain product per worker in a
+// library (2.08 ms); with 128 x 64 and two wavefronts a SIMD 2.20 ms, with 64 x 128 (tiles of 128 x 256) 2.59, with 64 x 64
+// (128 x 128, two workgroups a compute unit) 2.93.  At 2.16 ms it took 1.57 without turning tiles and writing them, 1.69
+// without loads, 2.07 without column sums.
 // Few steps: 15 x 1024 rows of 768 -> 2304, bf16 to fp32, 90 us = 0.60 PFLOP/s, in 405 tiles for 256 compute units; the results
 // are 106 MB that are written at one time at the end of a tile (65 us without it).  fp32 dY, three products for one: 60
 // uneven workers, 30011 rows of 1001 -> 509, 139 us = 0.22 PFLOP/s, 0.66 with the pieces.  7 x 32 rows of 48 -> 64: 7.2 us.
