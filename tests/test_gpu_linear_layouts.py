@@ -1,0 +1,89 @@
+"""Linear gradients where the layout of dy matters: a single row with any leading dimension.
+
+Bounds (u = 2^-24; a gradient stored in bf16 adds 2^-8 of its size): products are exact; a matrix instruction adds 16 rows of
+one piece of dy (one piece of bf16, three of fp32) to a sum, in at most two additions in turn of 2 u each; 32 more join
+lanes and parts; gamma P + beta b costs 4 u of its terms.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layers_oracle as lo
+from paper_2302_05865_amd import fa_checkpoint_pack, fa_linear_grad
+
+from gpu_util import announce
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+UB = 2.0 ** -8
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _host(t):
+    return t.detach().to(torch.float64).cpu().numpy()
+
+
+def _gradient(rng, rows, outputs):
+    return rng.normal(size=(rows, outputs)) * np.exp(rng.normal(size=(rows, 1))) * (rng.random((rows, 1)) > 0.1)
+
+
+def _pitched(values, dtype, offset, gap):
+    """`offset` elements into its memory, `gap` between rows, NaN in everything that is not an element."""
+    rows, width = values.shape
+    flat = torch.full((offset + rows * (width + gap) + 8,), float("nan"), dtype=TYPES[dtype], device="cuda")
+    view = flat.as_strided((rows, width), (width + gap, 1), offset)
+    view.copy_(torch.from_numpy(values))
+    return view
+
+
+def _check(dy, dtype, sizes, features, affine, grads, rng):
+    rows, outputs = dy.shape
+    p = len(sizes)
+    kept = fa_checkpoint_pack(torch.from_numpy(rng.normal(size=(rows, features)) + 0.3).float().cuda())
+    v = lo.unpack(kept.codes.cpu().numpy(), kept.exponents.cpu().numpy(), features)
+    gamma = beta = None
+    if affine:
+        gamma, beta = (torch.from_numpy(rng.normal(size=features)).float().cuda() for _ in range(2))
+    dweight = torch.full((p, outputs, features), -77.0, dtype=TYPES[grads], device="cuda")
+    dbias = torch.full((p, outputs), -77.0, dtype=TYPES[grads], device="cuda")
+    fa_linear_grad(dy, kept, sizes, dweight, dbias, gamma=gamma, beta=beta)
+    g, b = (_host(gamma), _host(beta)) if affine else (np.ones(features), np.zeros(features))
+    d, ends = _host(dy), np.concatenate([[0], np.cumsum(sizes)])
+    for w in range(p):
+        at, vw = d[ends[w]:ends[w + 1]], v[ends[w]:ends[w + 1]]
+        turns = 2 * U * ((3 if dtype == "f32" else 1) * sizes[w] / 8 + 32)
+        P, wb, most, mb = at.T @ vw, at.sum(0), np.abs(at).T @ np.abs(vw), np.abs(at).sum(0)
+        want = P * g + wb[:, None] * b
+        bound = np.abs(g) * turns * most + np.abs(b) * turns * mb[:, None] + 4 * U * (np.abs(P * g) + np.abs(wb[:, None] * b)) + 1e-38
+        got, bias = _host(dweight[w]), _host(dbias[w])
+        store = UB if grads == "bf16" else 0
+        assert (np.abs(got - want) <= bound + store * (np.abs(want) + bound)).all(), w
+        assert (np.abs(bias - wb) <= turns * mb + store * (np.abs(wb) + turns * mb) + 1e-38).all(), w
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sizes", [[1], [0, 1, 0]])
+@pytest.mark.parametrize("outputs", [2, 8, 63, 64, 200])
+def test_one_row_has_no_pitch(outputs, sizes, dtype):
+    """With one row its leading dimension has no meaning, whatever it is."""
+    announce("linear, one row", outputs, sizes, dtype)
+    rng = np.random.default_rng([outputs, len(sizes)])
+    values = torch.from_numpy(rng.normal(size=outputs)).to("cuda", TYPES[dtype])
+    for ld in (0, 1, outputs // 2, outputs - 1, outputs, 1 << 30):
+        for affine in (False, True):
+            _check(values.as_strided((1, outputs), (ld, 1)), dtype, sizes, 70, affine, "f32", np.random.default_rng(ld))
+    _check(values.view(outputs, 1).t(), dtype, sizes, 33, True, "f32", rng)
+    _check(values.expand(5, outputs)[:1], dtype, sizes, 33, True, "bf16", rng)
+
+
+def test_an_infinity_in_one_row_stays_with_its_output():
+    for dtype in TYPES.values():
+        dy = torch.ones(64, device="cuda", dtype=dtype)
+        dy[40] = float("inf")
+        kept = fa_checkpoint_pack(torch.ones((1, 40), device="cuda"))
+        dweight, dbias = torch.empty((1, 64, 40), device="cuda"), torch.empty((1, 64), device="cuda")
+        fa_linear_grad(dy.as_strided((1, 64), (1, 1)), kept, [1], dweight, dbias)
+        want = torch.ones(64, device="cuda")
+        want[40] = float("inf")
+        assert torch.equal(dbias[0], want) and torch.equal(dweight[0], want[:, None].expand(64, 40))
