@@ -449,7 +449,7 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
   float* block = bias + BM + wave * 32 * PITCH;
   const int i = i0 + wn + lane % LANES * 8, valid = a.features - i;
   float gamma[8], beta[8];
-  const bool affine = a.gamma && !part;
+  const bool affine = a.gamma && !part && all > 0;        // (a worker without rows: zeros, also where beta is infinite)
   if (affine) {
     fa_load8_param(a.gamma, a.param_bf16, i, valid, gamma);
     fa_load8_param(a.beta, a.param_bf16, i, valid, beta);
@@ -503,6 +503,7 @@ __global__ __launch_bounds__(kThreads) void fa_linear_grad_join_kernel(fa_linear
   const int64_t OI = (int64_t)a.outputs * a.features, all = OI + a.outputs;
   const int w = blockIdx.y;
   const float* part = a.partials + (int64_t)w * a.splits * all;
+  const bool affine = a.gamma && a.blocks.row0[w + 1] > a.blocks.row0[w];
   for (int64_t k = (int64_t)blockIdx.x * kThreads + threadIdx.x; k < all; k += (int64_t)gridDim.x * kThreads) {
     float s = add_up(part + k, all, a.splits);
     if (k >= OI) {
@@ -512,7 +513,7 @@ __global__ __launch_bounds__(kThreads) void fa_linear_grad_join_kernel(fa_linear
       else fa_store1(static_cast<float*>(a.dbias) + at, s);
       continue;
     }
-    if (a.gamma) {
+    if (affine) {
       const int64_t o = k / a.features;
       const int i = (int)(k - o * a.features);
       const float b = add_up(part + OI + o, all, a.splits);

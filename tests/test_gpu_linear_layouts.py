@@ -87,3 +87,23 @@ def test_an_infinity_in_one_row_stays_with_its_output():
         want = torch.ones(64, device="cuda")
         want[40] = float("inf")
         assert torch.equal(dbias[0], want) and torch.equal(dweight[0], want[:, None].expand(64, 40))
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_a_worker_without_rows_gets_zeros_whatever_the_parameters(bad):
+    """Its sums have no terms: an infinite gamma or beta does not come into them, in one part or joined from several."""
+    for sizes, outputs in (([0, 3, 0], 40), ([0, 9000], 8)):
+        for dtype in TYPES.values():
+            gen = torch.Generator(device="cuda").manual_seed(1)
+            dy = torch.randn(sum(sizes), outputs, generator=gen, device="cuda").to(dtype)
+            kept = fa_checkpoint_pack(torch.randn(sum(sizes), 70, generator=gen, device="cuda"))
+            gamma, beta = torch.ones(2, 70, device="cuda")
+            gamma[3], beta[5] = bad, bad
+            dweight, dbias = torch.full((len(sizes), outputs, 70), -77.0, device="cuda"), torch.full((len(sizes), outputs), -77.0, device="cuda")
+            fa_linear_grad(dy, kept, sizes, dweight, dbias, gamma=gamma, beta=beta)
+            for w, n in enumerate(sizes):
+                if n == 0:
+                    assert not dweight[w].any() and not dbias[w].any()
+                else:
+                    finite = torch.isfinite(dweight[w])
+                    assert not finite[:, [3, 5]].any() and int(finite.sum()) == outputs * 68
