@@ -1,4 +1,5 @@
-"""Linear gradients where the layout of dy matters: a single row with any leading dimension.
+"""Linear gradients where the layout of dy matters: a single row with any leading dimension, pitches and
+widths of either parity, rows of a step nearly 2^24 bytes apart.
 
 Bounds (u = 2^-24; a gradient stored in bf16 adds 2^-8 of its size): products are exact; a matrix instruction adds 16 rows of
 one piece of dy (one piece of bf16, three of fp32) to a sum, in at most two additions in turn of 2 u each; 32 more join
@@ -107,3 +108,28 @@ def test_a_worker_without_rows_gets_zeros_whatever_the_parameters(bad):
                 else:
                     finite = torch.isfinite(dweight[w])
                     assert not finite[:, [3, 5]].any() and int(finite.sum()) == outputs * 68
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("gap", [0, 1, 2, 3])
+@pytest.mark.parametrize("outputs", [2, 7, 50, 127, 129, 130])
+def test_pitches_of_either_parity(outputs, gap, dtype):
+    """Rows that begin at every place of a word and end there; one step and several, last steps of even and odd lengths."""
+    announce("linear, pitches", outputs, gap, dtype)
+    for sizes in ([1, 2], [63, 64], [65, 66, 0, 1], [127, 130, 191, 192], [129, 200]):
+        rng = np.random.default_rng([outputs, gap, sizes[0]])
+        for offset in (0, 1):
+            dy = _pitched(_gradient(rng, sum(sizes), outputs), dtype, offset, gap)
+            _check(dy, dtype, sizes, 70, offset == 1, "f32" if gap < 2 else "bf16", rng)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_farthest_rows_of_a_step(dtype):
+    """A pitch just below 2^22 elements: a step of fp32 is nearly 2^30 bytes long."""
+    announce("linear, far rows in a step", dtype)
+    rows, outputs, apart = 131, 24, (1 << 22) - 1
+    rng = np.random.default_rng(5)
+    flat = torch.full((rows * apart,), float("nan"), dtype=TYPES[dtype], device="cuda")
+    dy = flat.view(rows, apart)[:, :outputs]
+    dy.copy_(torch.from_numpy(_gradient(rng, rows, outputs)))
+    _check(dy, dtype, [rows - 2, 2], 40, True, "f32", rng)
