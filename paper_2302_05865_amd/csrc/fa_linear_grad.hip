@@ -12,6 +12,7 @@
 
 #include "fa.h"
 #include "fa_layers.h"
+#include "fa_linear_plan.h"
 
 namespace {
 
@@ -529,46 +530,8 @@ __global__ __launch_bounds__(kThreads) void fa_linear_grad_join_kernel(fa_linear
 
 namespace {
 
-// The two tiles of either type, and in how many parts the workers' rows are cut.  Time is counted in steps of a wide tile,
-// 2 us on a full card (bf16; 65536 x 4096 x 4096 takes 16 rounds of 64 of them): a narrow tile is a quarter of the
-// work, two of them share a compute unit, and the pair takes `step` of that (whole shapes: 65536 x 4096 x 4096 in 2.05 ms
-// wide, 2.93 ms narrow; 15 workers of 1024 rows, 768 -> 2304: 0.089 and 0.108 ms; fp32, 60 workers, 1001 -> 509: 0.140 and
-// 0.164 ms).  A round of workgroups costs `more` beside its steps, for the first loads and the last stores.  Parts are
-// joined at the rate of memory, behind one more launch.
-struct tile_kind {
-  int outputs, features, slots;
-  float step, more;
-};
-constexpr tile_kind kTiles[2][2] = {{{128, 256, 256, 1.f, 5.f}, {64, 128, 512, 0.56f, 3.f}},     // fp32 dY: wide, narrow
-                                    {{256, 256, 256, 1.f, 5.f}, {128, 128, 512, 0.69f, 3.f}}};   // bf16 dY
-constexpr int kParts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
-
-struct plan {
-  bool wide;
-  int splits;
-  int64_t tiles;   // of one worker
-};
-
-plan plan_of(const fa_row_blocks& b, int features, int outputs, int dtype) {
-  const int64_t mean = (b.row0[b.p] + b.p - 1) / b.p, steps = (mean + 63) / 64;
-  const double results = (double)b.p * outputs * features;
-  plan best = {};
-  double least = 0;
-  for (int narrow = 0; narrow < 2; ++narrow) {
-    const tile_kind& t = kTiles[dtype == FA_BF16][narrow];
-    const int64_t tiles = (int64_t)((outputs + t.outputs - 1) / t.outputs) * ((features + t.features - 1) / t.features);
-    for (const int parts : kParts) {
-      if (parts > 1 && parts > steps) break;
-      const int64_t rounds = (tiles * b.p * parts + t.slots - 1) / t.slots;
-      double cost = (double)rounds * ((double)((steps + parts - 1) / parts) * t.step + t.more);
-      if (parts > 1) cost += 1.5 + results * parts * (8 / 5.1e6 / 2);
-      if (best.splits == 0 || cost < least) {
-        least = cost;
-        best = {narrow == 0, parts, tiles};
-      }
-    }
-  }
-  return best;
+fa_linear_plan plan_of(const fa_row_blocks& b, int features, int outputs, int dtype) {
+  return fa_plan_linear_grad(b.row0[b.p], b.p, features, outputs, dtype == FA_BF16);
 }
 
 }  // namespace
@@ -579,7 +542,7 @@ size_t fa_linear_grad_partials(const fa_row_blocks& b, int features, int outputs
 }
 
 hipError_t fa_launch_linear_grad(fa_linear_grad_args a, int dtype, hipStream_t st) {
-  const plan c = plan_of(a.blocks, a.features, a.outputs, dtype);
+  const fa_linear_plan c = plan_of(a.blocks, a.features, a.outputs, dtype);
   a.splits = c.splits;
   const dim3 grid((unsigned)(c.tiles * a.blocks.p * c.splits));
   if (dtype == FA_F32) {

@@ -6,7 +6,7 @@ Listed once for the test of the rule (on the CPU) and for the kernels' test.
 WIDE_ONE_PART = {
     "bf16": [([130] * 38 + [0, 260], 520, 260),          # whole tiles and edges, even
              ([1, 0, 63, 64, 65] + [200] * 37, 515, 259),  # odd in both, ragged rows
-             ([150] * 42, 512, 257)],
+             ([150] * 42, 513, 257)],
     "f32": [([130] * 26 + [0, 260], 520, 260),
             ([1, 0, 63, 64, 65] + [200] * 23, 515, 259),
             ([150] * 28, 512, 257)],

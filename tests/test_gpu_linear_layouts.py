@@ -1,5 +1,5 @@
 """Linear gradients where the layout of dy matters: a single row with any leading dimension, pitches and
-widths of either parity, rows of a step nearly 2^24 bytes apart.
+widths of either parity, rows of a step nearly 2^24 bytes apart, tiles of either size.
 
 Bounds (u = 2^-24; a gradient stored in bf16 adds 2^-8 of its size): products are exact; a matrix instruction adds 16 rows of
 one piece of dy (one piece of bf16, three of fp32) to a sum, in at most two additions in turn of 2 u each; 32 more join
@@ -9,6 +9,7 @@ import numpy as np
 import pytest
 import torch
 
+from linear_shapes import WIDE_IN_PARTS, WIDE_ONE_PART
 from oracle import layers_oracle as lo
 from paper_2302_05865_amd import fa_checkpoint_pack, fa_linear_grad
 
@@ -133,3 +134,14 @@ def test_the_farthest_rows_of_a_step(dtype):
     dy = flat.view(rows, apart)[:, :outputs]
     dy.copy_(torch.from_numpy(_gradient(rng, rows, outputs)))
     _check(dy, dtype, [rows - 2, 2], 40, True, "f32", rng)
+
+
+@pytest.mark.parametrize("dtype,shape", [(t, s) for t in TYPES for s in WIDE_ONE_PART[t] + WIDE_IN_PARTS[t]],
+                         ids=lambda s: s if isinstance(s, str) else f"{len(s[0])}x{sum(s[0])}x{s[1]}x{s[2]}")
+def test_wide_tiles(shape, dtype):
+    sizes, features, outputs = shape
+    for gap, affine, grads in ((0, True, "f32"), (1, False, "bf16")):
+        announce("linear, wide tiles", len(sizes), sum(sizes), features, outputs, dtype, gap)
+        rng = np.random.default_rng([features, outputs, gap])
+        dy = _pitched(_gradient(rng, sum(sizes), outputs), dtype, gap, gap)
+        _check(dy, dtype, sizes, features, affine, grads, rng)
