@@ -455,8 +455,10 @@ fa_status fa_layer_norm_backward(const void* dy, int64_t lddy, const int64_t* si
  *   dweight_w = P_w,  or with gamma and beta (both or neither; the layer's input was
  *   v gamma + beta, a checkpointed layer norm's)  dweight_w[o, i] = gamma_i P_w[o, i] + beta_i b_w[o],
  *   dbias_w = b_w (may be NULL).
- * Products are exact (bf16 matrix core; fp32 dy in three exact pieces), sums fp32.  A worker
- * without rows gets zeros.  fa_linear_grad_workspace: bytes (may be 0), -1 for bad arguments.
+ * Products are exact on the bf16 matrix core: dy in bf16, or in fp32 as three pieces of eight
+ * bits.  The lowest ends at 2^-133, where bf16 ends, so dy below 2^-110 in size is cut off by less
+ * than 2^-133.  Sums are fp32; of fp32 dy the three pieces' products are added one by one, which is
+ * three times the additions of a plain fp32 product.  A worker without rows gets zeros.  fa_linear_grad_workspace: bytes (may be 0), -1 for bad arguments.
  */
 int64_t fa_linear_grad_workspace(const int64_t* sizes_host, int p, int features, int outputs,
                                  int dtype);

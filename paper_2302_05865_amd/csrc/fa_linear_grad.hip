@@ -4,7 +4,8 @@
 //   dW_w = gamma_i P_w + beta_i b_w[o]  (the layer's input was v gamma + beta)   or   dW_w = P_w,    db_w = b_w,
 //
 // where v are the checkpoint's values.  They have seven significant bits, so they are exact in bf16; dY is bf16, or fp32
-// cut exactly into three pieces of eight bits.  Every product on the bf16 matrix core is exact, sums are fp32.  The rows are
+// cut into three pieces of eight bits: exactly, but below 2^-110, where the lowest piece is cut off at 2^-133, the last place
+// of bf16.  Every product on the bf16 matrix core is exact, subnormal ones too, sums are fp32.  The rows are
 // the contracted index of both operands and lie far apart in memory; a lane of the matrix instruction takes eight
 // consecutive ones of a column, so tiles are turned on their way to LDS.
 #include <hip/hip_runtime.h>
@@ -21,8 +22,8 @@ constexpr int kThreads = 256;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-// x = h + m + l exactly, each with eight significant bits, h and m cut off (h of the largest finite value stays finite).
-// An infinity is h, with nothing left over; of a NaN, whatever h is, m is one.
+// x = h + m + l, each with eight significant bits (l to 2^-133 at the lowest), h and m cut off (h of the largest finite value
+// stays finite).  An infinity is h, with nothing left over; of a NaN, whatever h is, m is one.
 __device__ __forceinline__ void split3(float x, uint32_t* h, uint32_t* m, uint32_t* l) {
   const uint32_t hu = __float_as_uint(x) & 0xffff0000u;
   const float left = x - __uint_as_float(hu), r = __builtin_amdgcn_classf(x, 0x204) ? 0.f : left;

@@ -145,3 +145,24 @@ def test_wide_tiles(shape, dtype):
         rng = np.random.default_rng([features, outputs, gap])
         dy = _pitched(_gradient(rng, sum(sizes), outputs), dtype, gap, gap)
         _check(dy, dtype, sizes, features, affine, grads, rng)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_tiny_gradients(dtype):
+    """bf16 is exact down to its subnormals.  Of fp32 dy the lowest piece ends at 2^-133, the last place of bf16: exact from
+    2^-110 on, below that each dy cut off by less than 2^-133.  (Products are taken of one row: no sum rounds them, but the
+    three pieces' to 2 u each and the result's to half of 2^-149.)"""
+    rng = np.random.default_rng(8)
+    bits = 23 if dtype == "f32" else 7
+    for power in (-100, -109, -110, -111, -117, -118, -119, -125, -126, -127, -133, -140, -149):
+        values = np.concatenate([[1.0, 2 - 2.0 ** -bits], 1 + rng.integers(0, 1 << bits, size=60) * 2.0 ** -bits]) * 2.0 ** power
+        dy = torch.from_numpy(values).to("cuda", TYPES[dtype])[None]
+        d = _host(dy)[0]
+        kept = fa_checkpoint_pack(torch.from_numpy(rng.normal(size=(1, 33))).float().cuda())
+        v = lo.unpack(kept.codes.cpu().numpy(), kept.exponents.cpu().numpy(), 33)[0]
+        dweight, dbias = torch.empty((1, 62, 33), device="cuda"), torch.empty((1, 62), device="cuda")
+        fa_linear_grad(dy, kept, [1], dweight, dbias)
+        cut = np.where((np.abs(d) >= 2.0 ** -110) | (dtype == "bf16"), 0.0, 2.0 ** -133)
+        want = d[:, None] * v
+        assert (np.abs(_host(dweight)[0] - want) <= cut[:, None] * np.abs(v) + 6 * U * np.abs(want) + 2.0 ** -148).all(), power
+        assert (np.abs(_host(dbias)[0] - d) <= cut + 6 * U * np.abs(d) + 2.0 ** -148).all(), power
