@@ -146,9 +146,9 @@ extern "C" fa_status fa_linear_grad(const void* dy, int64_t lddy, const int64_t*
   if (need > 0 && (!workspace || ((uintptr_t)workspace & 15u) != 0 || workspace_bytes < need)) return FA_ERR_ARG;
   a.dy = dy; a.gamma = gamma; a.beta = beta; a.codes = codes; a.exponents = exponents;
   a.dweight = dweight; a.dbias = dbias; a.partials = static_cast<float*>(workspace);
-  // (rows that a step lacks are past the end of its buffer: the pitch of a single row, of no meaning to the caller and so
-  // perhaps 0, would put them inside that row)
-  a.lddy = rows == 1 ? outputs : lddy; a.lddweight = lddweight; a.lddbias = lddbias;
+  // (rows that a step lacks are past the end of its buffer.  The pitch of a single row, or of none, has no meaning to the
+  // caller and may be 0, which would put them inside that row)
+  a.lddy = rows <= 1 ? outputs : lddy; a.lddweight = lddweight; a.lddbias = lddbias;
   a.features = features; a.outputs = outputs; a.splits = 1; a.param_bf16 = param_dtype == FA_BF16; a.grad_bf16 = grad_dtype == FA_BF16;
   return fa_launch_linear_grad(a, dtype, (hipStream_t)stream) == hipSuccess ? FA_OK : FA_ERR_DEVICE;
 }

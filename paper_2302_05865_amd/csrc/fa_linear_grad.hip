@@ -199,7 +199,8 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
   const int b_col = tid % (BN / S::BC) * S::BC, b_piece = tid / (BN / S::BC);
   const int64_t steps = (end - begin + BK - 1) / BK;
   const bool odd = sizeof(T) == 2 && (a.outputs & 1);
-  const int64_t fast = a.lddy >= (1 << 22) || steps == 0 ? 0 : odd ? steps - 1 : steps;
+  const bool near = a.lddy < (1 << 22);                   // the bytes of a step, and one row more, fit in 31 bits
+  const int64_t fast = !near || steps == 0 ? 0 : odd ? steps - 1 : steps;
   const uint32_t a_off = (uint32_t)((int64_t)a_piece * 8 * a.lddy + (o0 + a_col < a.outputs ? a_col : 0)) * (uint32_t)sizeof(T);
   const int b_safe = i0 + b_col < pitch ? b_col : 0;
   const uint32_t b_off = (uint32_t)(b_piece * 8 * (int)pitch + b_safe);
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_g
   const unsigned char* at_dy = static_cast<const unsigned char*>(a.dy) + (begin * a.lddy + o0) * (int64_t)sizeof(T);
   const unsigned char* at_codes = reinterpret_cast<const unsigned char*>(a.codes) + begin * pitch + i0;
   const unsigned char* at_exponents = a.exponents + begin * epitch + (i0 >> 5);
-  const int row_dy = (int)a.lddy * (int)sizeof(T), row_codes = (int)pitch, row_exponents = (int)epitch;
+  const int row_dy = near ? (int)a.lddy * (int)sizeof(T) : 0, row_codes = (int)pitch, row_exponents = (int)epitch;
   // (ends of a step's buffers: of the last one's rows, of one row more than a step has where there is one more)
   const int rows_last = (int)(end - begin - (steps - 1) * BK), wide_dy = (a.outputs - o0) * (int)sizeof(T);
   const int last_dy = (rows_last - 1) * row_dy + wide_dy, full_dy = BK * row_dy + wide_dy;
