@@ -166,3 +166,12 @@ def test_tiny_gradients(dtype):
         want = d[:, None] * v
         assert (np.abs(_host(dweight)[0] - want) <= cut[:, None] * np.abs(v) + 6 * U * np.abs(want) + 2.0 ** -148).all(), power
         assert (np.abs(_host(dbias)[0] - d) <= cut + 6 * U * np.abs(d) + 2.0 ** -148).all(), power
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sizes", [[2500] + [0] * 63, [0] * 40 + [2001, 1, 0, 70], [3] * 30 + [3001]])
+def test_workers_of_very_different_lengths(sizes, dtype):
+    announce("linear, uneven workers", max(sizes), len(sizes), dtype)
+    rng = np.random.default_rng(len(sizes))
+    dy = _pitched(_gradient(rng, sum(sizes), 131), dtype, 1, 2)
+    _check(dy, dtype, sizes, 150, True, "f32", rng)
