@@ -2,7 +2,9 @@
 
 The functions check tensor types and shapes, take torch's current stream of the tensors' device,
 allocate outputs and workspace from torch's allocator (so a call is as safe on a side stream as
-any torch operation) and forward to ``libfa.so``.
+any torch operation) and forward to ``libfa.so``.  They are no autograd functions: what they
+return has no graph, whether or not an input requires a gradient, and they put gradients where
+they are told to.
 """
 from __future__ import annotations
 
@@ -99,7 +101,8 @@ def _call(name: str, device, *args) -> None:
 class Checkpoint:
     """An activation [rows, features] in 8 bits: ``codes`` (int8, rows padded to whole blocks of
     32 features) and ``exponents`` (uint8, one for each block, rows padded to multiples of four).
-    ``codes * 2**(exponents - 127)`` are its values; the layout is that of include/fa.h."""
+    ``codes * 2**(exponents - 127)`` are its values, exponents 1 to 248, and NaN where the
+    exponent is 255; the layout is that of include/fa.h."""
 
     __slots__ = ("codes", "exponents", "features")
 

@@ -176,8 +176,8 @@ __device__ __forceinline__ void each_piece(F f) {
 // sum of squares costs no second pass; the next row's loads stand ahead of this one's reductions, and nothing a wavefront
 // waits for is behind a branch (the waits would be for everything in flight).
 // Rows of more than 256 features are read and written as buffers of their own length, in which lanes past the end do nothing.
-// Measured: 65536 x 4096 bf16 217 us = 4.95 TB/s (a copy: 5.13), 15360 x 768 bf16 with a checkpoint 15.3 us = 3.9 TB/s, one
-// row of 768 2.9 us, which is a launch and one turn to memory and back.
+// Measured: 65536 x 4096 bf16 220 us = 4.9 TB/s (a copy: 5.13), 32768 x 4096 fp32 194 us = 5.5 TB/s, 15360 x 768 bf16 with a
+// checkpoint 14.3 us = 4.2 TB/s, one row of 768 2.7 us, which is a launch and one turn to memory and back.
 template <typename T, bool KEEP, int L, int NC, int W>
 __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_kernel(fa_norm_args a) {
   static_assert(W == 1 || L == 64, "a team of several wavefronts uses all their lanes");
@@ -313,8 +313,8 @@ __device__ __forceinline__ int worker_of(const int* first, int p, int k) {
 // the lane that has the feature, all its rows long.  That costs registers (two sums and gamma for every feature of a lane),
 // so wide rows are spread over more wavefronts than in the forward pass.  Both sums over features go through one reduction
 // and one barrier; no atomics: the sums come out the same at every call.  Measured: 65536 x 4096 bf16 from the checkpoint
-// 278 us = 4.86 TB/s (eight features a lane in eight wavefronts 440, gamma in LDS 421), 15360 x 768 bf16 with residual
-// 18.9 us = 4.4 TB/s, 1001 x 257 fp32 5.3 us.
+// 280 us = 4.8 TB/s (eight features a lane in eight wavefronts 440, gamma in LDS 421), from x 334 us = 4.8 TB/s, 32768 x 4096
+// fp32 from x 311 us = 5.2 TB/s, 15360 x 768 bf16 with residual 18.4 us = 4.5 TB/s, 1001 x 257 fp32 5.2 us.
 template <typename T, bool KEPT, int L, int NC, int W>
 __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_backward_kernel(fa_norm_grad_args a, norm_chunks ch) {
   constexpr int TL = L * W;
@@ -508,7 +508,7 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : kThreads) void fa_layer_norm_backw
 }
 
 // dgamma (blockIdx.z = 0) and dbeta (1) of one worker: its chunks' shares in eight interleaved sums, these in their order.
-// Latency: a thread has eight loads in flight.  768 chunks of 4096 features (25 MB, from the cache) 8.8 us, of 768 3.9 us.
+// Latency: a thread has eight loads in flight.  768 chunks of 4096 features (25 MB, from the cache) 7.2 us, of 768 3.9 us.
 __global__ __launch_bounds__(kThreads) void fa_layer_norm_grads_kernel(fa_norm_grad_args a, norm_chunks ch) {
   constexpr int GROUPS = 8, COLUMNS = kThreads / GROUPS, DEEP = 8;
   __shared__ float red[GROUPS][COLUMNS];
@@ -540,7 +540,7 @@ __global__ __launch_bounds__(kThreads) void fa_layer_norm_grads_kernel(fa_norm_g
   }
 }
 
-// Any activation to a checkpoint: one pass bound by memory, every element read once.  9999 x 1111 fp32 10.9 us = 5.1 TB/s.
+// Any activation to a checkpoint: one pass bound by memory, every element read once.  9999 x 1111 fp32 10.1 us = 5.5 TB/s.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void fa_checkpoint_pack_kernel(const T* x, int64_t ldx, int64_t rows, int D, int8_t* codes,
                                                                       uint8_t* exponents) {
@@ -561,7 +561,7 @@ __global__ __launch_bounds__(kThreads) void fa_checkpoint_pack_kernel(const T* x
   }
 }
 
-// And back, a thread for every eight codes: bound by its writes.  65536 x 4096 to bf16 157 us = 5.2 TB/s.
+// And back, a thread for every eight codes: bound by its writes.  65536 x 4096 to bf16 155 us = 5.2 TB/s.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void fa_checkpoint_unpack_kernel(const int8_t* codes, const uint8_t* exponents, int64_t rows,
                                                                         int D, T* x, int64_t ldx) {

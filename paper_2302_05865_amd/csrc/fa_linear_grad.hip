@@ -46,7 +46,8 @@ __device__ __forceinline__ uint32_t upper_halves(uint32_t a, uint32_t b) { retur
 // every output (feature), the BK values of the contracted index in pieces of 8, which is what a lane of the matrix
 // instruction takes with one 16-byte read.  Piece c of column j lies at place c ^ swizzle(j): 16 lanes that read one
 // piece of 16 neighbouring columns, and 8 that write one piece of every second, fourth or eighth column (as wide as a
-// thread's unit is), meet no bank twice.
+// thread's unit is), meet no bank twice (65536 x 4096 x 4096: 4.2e6 cycles of conflicts to 2.9e8 in which LDS works, all of
+// them in the reads of finished results; with column / 8 in place of column / 16 in swizzle() 1.39e8).
 namespace {
 
 template <typename T, int BM, int BN, int BK>
@@ -167,9 +168,10 @@ __device__ __forceinline__ float add8(bf16x8 v, float s) {
 // library (2.08 ms); with 128 x 64 and two wavefronts a SIMD 2.20 ms, with 64 x 128 (tiles of 128 x 256) 2.59, with 64 x 64
 // (128 x 128, two workgroups a compute unit) 2.93.  At 2.16 ms it took 1.57 without turning tiles and writing them, 1.69
 // without loads, 2.07 without column sums.
-// Few steps: 15 x 1024 rows of 768 -> 2304, bf16 to fp32, 90 us = 0.60 PFLOP/s, in 405 tiles for 256 compute units; the results
+// Few steps: 15 x 1024 rows of 768 -> 2304, bf16 to fp32, 86 us = 0.63 PFLOP/s, in 405 tiles for 256 compute units; the results
 // are 106 MB that are written at one time at the end of a tile (65 us without it).  fp32 dY, three products for one: 60
-// uneven workers, 30011 rows of 1001 -> 509, 139 us = 0.22 PFLOP/s, 0.66 with the pieces.  7 x 32 rows of 48 -> 64: 7.2 us.
+// uneven workers, 30011 rows of 1001 -> 509, 133 us = 0.23 PFLOP/s, 0.69 with the pieces.  7 x 32 rows of 48 -> 64: 7.4 us.  (Kernels
+// alone, on a card that has been at work for some milliseconds.)
 template <typename T, int BM, int BN, int BK>
 __global__ __launch_bounds__(kThreads, 1) void fa_linear_grad_kernel(fa_linear_grad_args a) {
   using S = tile<T, BM, BN, BK>;
